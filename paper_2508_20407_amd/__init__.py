@@ -4,6 +4,9 @@
 that live on the GPU ([B,H,rows,D], last axis contiguous), marshal their addresses and strides
 into the C-ABI call of the same name and return the output tensor.  All arithmetic happens in
 the library's HIP kernels.
+
+``tlin_rope``, ``tlin_paged_append``, ``tlin_paged_attn`` and ``tlin_pages_*`` do the same for a paged
+cache (see ``paged.py``).
 """
 from __future__ import annotations
 
@@ -11,6 +14,8 @@ from . import binding
 from .binding import (TLIN_BF16, TLIN_COMBINE_JOINT, TLIN_COMBINE_SUM, TLIN_F32, TlinError, TlinParams)
 
 __all__ = ["tlin_history_attn", "tlin_window_causal_attn", "tlin_layer_attn", "tlin_layer_attn_static_ws", "tlin_slide_layer_attn", "Workspace", "params_for",
+           "tlin_rope", "rope_frequencies", "tlin_paged_append", "tlin_paged_attn", "tlin_pages_reserve", "tlin_pages_fork",
+           "tlin_pages_free", "tlin_pages_compact", "tlin_pages_copy",
            "TLIN_F32", "TLIN_BF16", "TLIN_COMBINE_SUM", "TLIN_COMBINE_JOINT", "TlinError", "TlinParams",
            "binding"]
 
@@ -195,3 +200,7 @@ def tlin_slide_layer_attn(q, k_hist, v_hist, k_win, v_win, chunk, *, combine=TLI
                                       v_win.data_ptr(), o.data_ptr(), ws or None, nb, stream)
     binding._check(st, "tlin_slide_layer_attn")
     return o
+
+
+from .paged import (rope_frequencies, tlin_paged_append, tlin_paged_attn, tlin_pages_compact, tlin_pages_copy,  # noqa: E402
+                    tlin_pages_fork, tlin_pages_free, tlin_pages_reserve, tlin_rope)

@@ -18,7 +18,10 @@ TLIN_F32, TLIN_BF16 = 0, 1
 TLIN_COMBINE_SUM, TLIN_COMBINE_JOINT = 0, 1
 
 EXPORTS = ("tlin_workspace_bytes", "tlin_num_splits", "tlin_history_attn", "tlin_window_causal_attn",
-           "tlin_layer_attn", "tlin_layer_attn_static_ws", "tlin_slide_workspace_bytes", "tlin_slide_layer_attn", "tlin_profile_enable", "tlin_profile_read", "tlin_profile_stream_read", "tlin_status_string", "tlin_version")
+           "tlin_layer_attn", "tlin_layer_attn_static_ws", "tlin_slide_workspace_bytes", "tlin_slide_layer_attn", "tlin_profile_enable", "tlin_profile_read", "tlin_profile_stream_read", "tlin_status_string", "tlin_version",
+           "tlin_rope", "tlin_rope_frequencies", "tlin_paged_append", "tlin_paged_workspace_bytes", "tlin_paged_attn",
+           "tlin_pages_free", "tlin_pages_fork", "tlin_pages_workspace_bytes", "tlin_pages_reserve", "tlin_pages_compact",
+           "tlin_pages_copy")
 
 
 class TlinParams(ctypes.Structure):
@@ -30,6 +33,48 @@ class TlinParams(ctypes.Structure):
         ("q_stride", ctypes.c_int64 * 3), ("kh_stride", ctypes.c_int64 * 3), ("vh_stride", ctypes.c_int64 * 3),
         ("kw_stride", ctypes.c_int64 * 3), ("vw_stride", ctypes.c_int64 * 3), ("o_stride", ctypes.c_int64 * 3),
     ]
+
+
+class TlinRopeParams(ctypes.Structure):
+    """Mirror of ``tlin_rope_params`` in include/tlinpaged.h."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "rows", "D", "rot", "interleaved", "transpose", "dtype")] + [
+        ("amplitude", ctypes.c_float), ("pos_stride", ctypes.c_int32),
+        ("x_stride", ctypes.c_int64 * 3), ("y_stride", ctypes.c_int64 * 3)]
+
+
+class TlinPagedParams(ctypes.Structure):
+    """Mirror of ``tlin_paged_params`` in include/tlinpaged.h."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("S", "T", "H", "HK", "D", "page_rows", "table_width", "num_pages", "max_rows",
+                                             "dtype", "out_dtype", "causal")] + [
+        ("scale", ctypes.c_float), ("table_stride", ctypes.c_int32),
+        ("q_stride", ctypes.c_int64 * 2), ("o_stride", ctypes.c_int64 * 2), ("k_stride", ctypes.c_int64 * 2),
+        ("v_stride", ctypes.c_int64 * 2), ("kp_stride", ctypes.c_int64 * 3), ("vp_stride", ctypes.c_int64 * 3)]
+
+
+class TlinBookParams(ctypes.Structure):
+    """Mirror of ``tlin_book_params`` in include/tlinpaged.h."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("S", "table_width", "num_pages", "page_rows", "table_stride")]
+
+
+class TlinCacheParams(ctypes.Structure):
+    """Mirror of ``tlin_cache_params`` in include/tlinpaged.h."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("layers", "num_pages", "HK", "page_rows", "D", "dtype")] + [
+        ("layer_stride", ctypes.c_int64 * 2), ("a_stride", ctypes.c_int64 * 3), ("b_stride", ctypes.c_int64 * 3)]
+
+
+# how a parameter structure is filled, as bytes in one go: assigning array fields builds temporary arrays
+ROPE_LAYOUT = struct.Struct("=8ifi6q")
+PAGED_LAYOUT = struct.Struct("=12ifi8q6q")
+BOOK_LAYOUT = struct.Struct("=5i")
+CACHE_LAYOUT = struct.Struct("=6i8q")
+TLIN_ROPE_PLAIN, TLIN_ROPE_LINEAR, TLIN_ROPE_BASE, TLIN_ROPE_PARTS = range(4)
+
+
+def packed(cls, layout, *values):
+    """A parameter structure with its fields in order."""
+    p = cls()
+    layout.pack_into(p, 0, *values)
+    return p
 
 
 _STRIDES = struct.Struct("=3q")
@@ -80,6 +125,22 @@ def lib() -> ctypes.CDLL:
         L.tlin_status_string.argtypes = [ctypes.c_int]
         L.tlin_version.restype = ctypes.c_int32
         L.tlin_version.argtypes = []
+        rp, gp, bp, cp = (ctypes.POINTER(c) for c in (TlinRopeParams, TlinPagedParams, TlinBookParams, TlinCacheParams))
+        i32, f64 = ctypes.c_int32, ctypes.c_double
+        for name, res, args in (
+                ("tlin_rope", ctypes.c_int, [rp, vp, vp, vp, vp, vp]),
+                ("tlin_rope_frequencies", ctypes.c_int, [i32, f64, i32, f64, f64, f64, f64, ctypes.POINTER(f64), ctypes.POINTER(f64)]),
+                ("tlin_paged_append", ctypes.c_int, [gp, rp] + [vp] * 11),
+                ("tlin_paged_workspace_bytes", sz, [gp]),
+                ("tlin_paged_attn", ctypes.c_int, [gp] + [vp] * 9 + [sz, vp]),
+                ("tlin_pages_free", ctypes.c_int, [bp, vp, vp, vp, vp, i32, vp]),
+                ("tlin_pages_fork", ctypes.c_int, [bp, vp, vp, vp, vp, vp, i32, vp, vp]),
+                ("tlin_pages_workspace_bytes", sz, [bp]),
+                ("tlin_pages_reserve", ctypes.c_int, [bp] + [vp] * 8 + [sz, vp]),
+                ("tlin_pages_compact", ctypes.c_int, [bp] + [vp] * 7 + [sz, vp]),
+                ("tlin_pages_copy", ctypes.c_int, [cp, vp, vp, vp, vp, i32, vp])):
+            f = getattr(L, name)
+            f.restype, f.argtypes = res, args
         _lib = L
     return _lib
 

@@ -4,11 +4,14 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libtlinattn.so")
 SRC = os.path.join(HERE, "csrc", "tlinattn.hip")
+# the paged cache: a translation unit of its own, linked behind the first
+PAGED_SRC = os.path.join(HERE, "csrc_paged", "paged.hip")
 
 # Packed-fp32 VALU instructions are switched off for all device code.
 HIPCC_FLAGS = [
@@ -19,14 +22,25 @@ HIPCC_FLAGS = [
 
 
 def build(verbose: bool = False, extra=()) -> str:
-    cmd = ["hipcc", *HIPCC_FLAGS, *extra, "-I", os.path.join(ROOT, "include"),
-           "-I", os.path.join(HERE, "csrc"), SRC, "-o", LIB_PATH]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    inc = ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"), "-I", os.path.join(HERE, "csrc_paged")]
+    with tempfile.TemporaryDirectory() as tmp:
+        objs, jobs = [], []
+        for src in (SRC, PAGED_SRC):
+            objs.append(os.path.join(tmp, os.path.basename(src) + ".o"))
+            cmd = ["hipcc", *(f for f in HIPCC_FLAGS if f != "-shared"), *extra, *inc, "-c", src, "-o", objs[-1]]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            jobs.append(subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True))
+        results = [(job.communicate()[1], job.returncode) for job in jobs]      # both run on side by side
+        link = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB_PATH]
+        if all(rc == 0 for _, rc in results):
+            if verbose:
+                print(" ".join(link), flush=True)
+            res = subprocess.run(link, capture_output=True, text=True)
+            results.append((res.stderr, res.returncode))
     # the host pass does not know the device-only target feature and says so: harmless
-    err = "\n".join(l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
+    err = "\n".join(l for text, _ in results for l in text.splitlines() if "packed-fp32-ops" not in l)
+    if any(rc != 0 for _, rc in results):
         raise RuntimeError("hipcc failed:\n" + err)
     if verbose and err.strip():
         print(err, file=sys.stderr)

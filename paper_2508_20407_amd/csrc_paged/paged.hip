@@ -1,0 +1,469 @@
+// libtlinattn: entry points of the paged cache (see include/tlinpaged.h).  gfx950 only.
+#include "host.h"
+#include "attn_paged_bf16.h"
+#include "attn_paged_f32.h"
+#include "attn_paged_merge.h"
+#include "pages.h"
+#include "rope.h"
+
+using namespace tlin;
+
+namespace {
+
+// ---- rotary positions and append
+
+int power_of_two(int n)
+{
+    int p = 1;
+    while (p < n) p *= 2;
+    return p;
+}
+
+// Elements that a thread takes of each half of its pairs: whole pieces where the halves are whole pieces, else two
+// elements or one.
+int rope_elements(int rot, bool interleaved, int eb)
+{
+    const int per16 = 16 / eb, half = rot / 2;
+    if (interleaved || half % per16 == 0) return per16;
+    return half % 2 == 0 ? 2 : 1;
+}
+
+// Lanes of a rotated row (a power of two, the units of the row or more) and tokens of a workgroup: as many as give
+// each thread about four pieces, but a thousand workgroups where there are tokens for them (a hundred tokens would
+// otherwise sit on a few compute units), and few enough that r / H is exact in fp32.
+void rope_shape(RopeArgs &a, int E, bool interleaved, int heads)
+{
+    const int units = interleaved ? (a.D + E - 1) / E : a.rot / 2 / E + (a.D - a.rot + E - 1) / E;
+    a.lanes = power_of_two(units);
+    const int64_t work = (int64_t)heads * a.lanes;
+    int64_t tb = 1024 / work;
+    if (tb > a.tokens / 1024) tb = a.tokens / 1024;
+    if (tb > kRopeTokens) tb = kRopeTokens;
+    a.TB = tb < 1 ? 1 : (int)tb;
+}
+
+template <typename T, bool APPEND>
+const void *rope_kernel_for(int E, bool interleaved)
+{
+    constexpr int EP = 16 / sizeof(T);
+    if (interleaved) return (const void *)rope_kernel<T, EP, true, APPEND>;
+    return E == EP ? (const void *)rope_kernel<T, EP, false, APPEND>
+           : E == 2 ? (const void *)rope_kernel<T, 2, false, APPEND> : (const void *)rope_kernel<T, 1, false, APPEND>;
+}
+
+template <bool APPEND>
+tlin_status launch_rope(const RopeArgs &a, int dtype, int E, bool interleaved, hipStream_t st)
+{
+    tlin_status s = check_device();
+    if (s) return s;
+    const void *kernel = dtype == TLIN_F32 ? rope_kernel_for<float, APPEND>(E, interleaved) : rope_kernel_for<__bf16, APPEND>(E, interleaved);
+    return launch_kernel(kernel, dim3((a.tokens + a.TB - 1) / a.TB), dim3(256), 0, st, a);
+}
+
+tlin_status check_rope(const tlin_rope_params *p)
+{
+    if (p->rot < 2 || p->rot > p->D || p->rot % 2) return TLIN_ERR_INVALID_ARG;
+    if (!isfinite(p->amplitude)) return TLIN_ERR_INVALID_ARG;
+    return TLIN_OK;
+}
+
+// ---- sizes that the paged calls share
+tlin_status check_paged(const tlin_paged_params *p)
+{
+    if (!p) return TLIN_ERR_INVALID_ARG;
+    if (p->S < 1 || p->T < 1 || p->H < 1 || p->HK < 1 || p->T > kMaxRows) return TLIN_ERR_INVALID_ARG;
+    if (p->H % p->HK || p->H / p->HK > 64 || p->H > 1 << 20 || p->S > 1 << 24) return TLIN_ERR_INVALID_ARG;
+    if (!good_dim(p->D)) return TLIN_ERR_UNSUPPORTED;
+    if (!good_page_rows(p->page_rows)) return TLIN_ERR_UNSUPPORTED;
+    if (p->table_width < 1 || p->num_pages < 1 || (int64_t)p->table_width * p->page_rows > kMaxRows) return TLIN_ERR_INVALID_ARG;
+    if (p->max_rows < 1 || p->max_rows > p->T) return TLIN_ERR_INVALID_ARG;
+    if (!is_type(p->dtype) || !is_type(p->out_dtype)) return TLIN_ERR_INVALID_ARG;
+    if (p->table_stride != 0 && p->table_stride < p->table_width) return TLIN_ERR_INVALID_ARG;
+    const int eb = bytes_of(p->dtype);
+    tlin_status st;
+    if ((st = check_strides(p->kp_stride, p->D, eb)) || (st = check_strides(p->vp_stride, p->D, eb))) return st;
+    return TLIN_OK;
+}
+
+tlin_status check_book(const tlin_book_params *p)
+{
+    if (!p || p->S < 1 || p->S > 1 << 24 || p->table_width < 1 || p->num_pages < 1 || p->num_pages > kMaxRows) return TLIN_ERR_INVALID_ARG;
+    if (!good_page_rows(p->page_rows)) return TLIN_ERR_UNSUPPORTED;
+    if ((int64_t)p->table_width * p->page_rows > kMaxRows) return TLIN_ERR_INVALID_ARG;
+    if (p->table_stride != 0 && p->table_stride < p->table_width) return TLIN_ERR_INVALID_ARG;
+    return TLIN_OK;
+}
+
+BookArgs book_args(const tlin_book_params *p)
+{
+    BookArgs a = {};
+    a.S = p->S; a.M = p->table_width; a.P = p->num_pages; a.lr = log2_of(p->page_rows);
+    a.stride = p->table_stride ? p->table_stride : p->table_width;
+    return a;
+}
+
+// ---- attention
+
+// Waves of a workgroup (32 rows each) and what follows from them.
+struct PagedShape { int nw, shares, dk, tb; int bm() const { return nw * 32; } };
+
+int group_of(const tlin_paged_params *p) { return p->H / p->HK; }
+
+// As few waves as hold a sequence's rows, (new row, query head) pairs, up to eight: two at least, so that one loads beside the
+// one that computes where rows are few, four where rows of 64 elements leave registers for three workgroups to a
+// compute unit.  Shares: the workgroups that the chip holds at once, by registers and LDS (bf16: 64 KB of tiles at
+// 128 columns, one workgroup of eight waves or two smaller ones to a compute unit; half of that at 64).
+PagedShape paged_shape(const tlin_paged_params *p)
+{
+    const int64_t rows = (int64_t)p->max_rows * group_of(p);
+    const bool bf = p->dtype == TLIN_BF16;
+    PagedShape s;
+    s.dk = p->D <= 64 ? 64 : 128;
+    s.nw = rows <= 64 ? 2 : rows <= 128 || s.dk == 64 || !bf ? 4 : 8;
+    s.shares = s.nw == 8 ? kNumCU : s.dk == 128 ? 2 * kNumCU : 3 * kNumCU;
+    s.tb = s.bm() / group_of(p);
+    return s;
+}
+
+struct PagedWorkspace { float *O, *M, *L; };
+size_t paged_workspace(const PagedShape &s, void *ws, PagedWorkspace &w)
+{
+    const size_t rows = 2 * (size_t)s.shares * s.bm();
+    w.O = (float *)ws;
+    w.M = w.O + rows * s.dk;
+    w.L = w.M + rows;
+    return (rows * s.dk + 2 * rows) * sizeof(float);
+}
+
+template <int DU, int NW, bool NT>
+tlin_status launch_paged_bf16(const PagedArgs &a, hipStream_t st)
+{
+    const void *kernel = (const void *)paged_bf16_kernel<DU, NW, NT>;
+    constexpr int lds = PagedBf16<DU, NW, NT>::LDS_BYTES;
+    static std::atomic<uint64_t> allowed{0};
+    tlin_status s = allow_lds(kernel, lds, allowed);
+    return s ? s : launch_kernel(kernel, dim3(a.shares), dim3(NW * 64), lds, st, a);
+}
+template <int DU, int NW>
+tlin_status launch_paged_f32(const PagedArgs &a, hipStream_t st)
+{
+    const void *kernel = (const void *)paged_f32_kernel<DU, NW>;
+    constexpr int lds = PagedF32<DU, NW>::LDS_BYTES;
+    static std::atomic<uint64_t> allowed{0};
+    tlin_status s = allow_lds(kernel, lds, allowed);
+    return s ? s : launch_kernel(kernel, dim3(a.shares), dim3(NW * 64), lds, st, a);
+}
+template <int DU>
+tlin_status launch_paged(const PagedArgs &a, const PagedShape &s, bool bf, bool nt, hipStream_t st)
+{
+    if (!bf) return s.nw == 2 ? launch_paged_f32<DU, 2>(a, st) : launch_paged_f32<DU, 4>(a, st);
+    if (s.nw == 2) return nt ? launch_paged_bf16<DU, 2, true>(a, st) : launch_paged_bf16<DU, 2, false>(a, st);
+    if (s.nw == 4) return launch_paged_bf16<DU, 4, false>(a, st);
+    if constexpr (DU > 64) return launch_paged_bf16<DU, 8, false>(a, st);
+    return TLIN_ERR_UNSUPPORTED;      // (not reached: eight waves are for rows of 128)
+}
+
+template <int DK, int BM, int BN>
+tlin_status launch_paged_merge(const PagedArgs &a, bool many, hipStream_t st)
+{
+    const void *kernel = many ? (const void *)paged_merge_kernel<DK, BM, BN, 8> : (const void *)paged_merge_kernel<DK, BM, BN, 1>;
+    const int rpb = kMergeThreads / (DK / 4) / (many ? 8 : 1);
+    const int rows = a.TB * a.G;
+    int blocks = (rows + rpb - 1) / rpb;
+    if (blocks > 8) blocks = 8;
+    return launch_kernel(kernel, dim3(a.shares - 1, blocks), dim3(kMergeThreads), 0, st, a);
+}
+
+int page_blocks(const tlin_book_params *p) { return (p->num_pages + kPagesPerBlock - 1) / kPagesPerBlock; }
+
+}  // namespace
+
+extern "C" {
+
+tlin_status tlin_rope(const tlin_rope_params *p, const void *x, void *y, const int32_t *pos, const double *freqs, void *stream)
+{
+    if (!p || p->B < 1 || p->H < 1 || p->rows < 1 || p->H > 1 << 20) return TLIN_ERR_INVALID_ARG;
+    if ((int64_t)p->B * p->rows > kMaxRows) return TLIN_ERR_INVALID_ARG;
+    if (!good_dim(p->D)) return TLIN_ERR_UNSUPPORTED;
+    if (!is_type(p->dtype) || p->pos_stride < 0) return TLIN_ERR_INVALID_ARG;
+    tlin_status st = check_rope(p);
+    if (st) return st;
+    const int eb = bytes_of(p->dtype);
+    if ((st = check_strides(p->x_stride, p->D, eb)) || (st = check_strides(p->y_stride, p->D, eb))) return st;
+    if (!x || !y || !pos || !freqs) return TLIN_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(y, 16) || !aligned(pos, 4) || !aligned(freqs, 8)) return TLIN_ERR_INVALID_ARG;
+    RopeArgs a = {};
+    int64_t xs[3], ys[3];
+    const int64_t sizes[2] = {p->H, p->rows};
+    resolve(p->x_stride, sizes, p->D, xs);
+    resolve(p->y_stride, sizes, p->D, ys);
+    if (x == y && (xs[0] != ys[0] || xs[1] != ys[1] || xs[2] != ys[2])) return TLIN_ERR_INVALID_ARG;
+    a.q = {x, y, xs[1], xs[2], ys[1], ys[2], p->H};
+    a.q_sb = xs[0]; a.qy_sb = ys[0];
+    a.pos = pos; a.pos_stride = p->pos_stride;
+    a.rows = p->rows; a.tokens = p->B * p->rows;
+    a.D = p->D; a.rot = p->rot; a.amplitude = p->amplitude; a.negate = p->transpose != 0;
+    a.freqs = freqs;
+    const int E = rope_elements(p->rot, p->interleaved, eb);
+    rope_shape(a, E, p->interleaved, p->H);
+    return launch_rope<false>(a, p->dtype, E, p->interleaved != 0, (hipStream_t)stream);
+}
+
+tlin_status tlin_rope_frequencies(int32_t rot, double base, int32_t scaling, double factor, double trained, double slow,
+                                  double fast, double *freqs, double *amplitude)
+{
+    if (rot < 2 || rot % 2 || rot > 128 || !freqs || !(base > 0) || !isfinite(base)) return TLIN_ERR_INVALID_ARG;
+    if (scaling < TLIN_ROPE_PLAIN || scaling > TLIN_ROPE_PARTS) return TLIN_ERR_INVALID_ARG;
+    if (scaling != TLIN_ROPE_PLAIN && (!(factor >= 1) || !isfinite(factor))) return TLIN_ERR_INVALID_ARG;
+    if (scaling == TLIN_ROPE_BASE && rot < 4) return TLIN_ERR_INVALID_ARG;
+    if (scaling == TLIN_ROPE_PARTS && (!(trained > 0) || !isfinite(trained) || !(slow >= 0) || !(fast > slow) || !isfinite(fast)))
+        return TLIN_ERR_INVALID_ARG;
+    if (scaling == TLIN_ROPE_BASE) base *= pow(factor, (double)rot / (rot - 2));
+    for (int i = 0; i < rot / 2; ++i) {
+        double f = pow(base, -2.0 * i / rot);
+        if (scaling == TLIN_ROPE_LINEAR) f /= factor;
+        if (scaling == TLIN_ROPE_PARTS) {
+            const double turns = f * trained / 6.283185307179586477;
+            double keep = (turns - slow) / (fast - slow);
+            keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
+            f = f * keep + f / factor * (1 - keep);
+        }
+        freqs[i] = f;
+    }
+    if (amplitude) *amplitude = scaling == TLIN_ROPE_PARTS ? 0.1 * log(factor) + 1.0 : 1.0;
+    return TLIN_OK;
+}
+
+tlin_status tlin_paged_append(const tlin_paged_params *p, const tlin_rope_params *r, const void *q, void *q_out,
+                              const void *k, const void *v, void *k_pages, void *v_pages, const int32_t *table,
+                              const int32_t *lens, const int32_t *starts, const double *freqs, void *stream)
+{
+    tlin_status st = check_paged(p);
+    if (st) return st;
+    const int eb = bytes_of(p->dtype);
+    if ((st = check_strides(p->k_stride, p->D, eb)) || (st = check_strides(p->v_stride, p->D, eb))) return st;
+    if (!k || !v || !k_pages || !v_pages || !table || !lens || !starts) return TLIN_ERR_INVALID_ARG;
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16)) return TLIN_ERR_INVALID_ARG;
+    if (!aligned(table, 4) || !aligned(lens, 4) || !aligned(starts, 4)) return TLIN_ERR_INVALID_ARG;
+    if (!q != !q_out) return TLIN_ERR_INVALID_ARG;
+    RopeArgs a = {};
+    bool inter = true;       // nothing is rotated: whole pieces, none of which holds pairs
+    a.D = p->D;
+    int64_t s1[2], s2[2], s3[3];
+    const int64_t rows[1] = {p->T}, page[2] = {p->HK, p->page_rows};
+    if (r) {
+        tlin_rope_params c = *r;
+        c.D = p->D;
+        if ((st = check_rope(&c))) return st;
+        if (!freqs || !aligned(freqs, 8)) return TLIN_ERR_INVALID_ARG;
+        inter = r->interleaved != 0;
+        a.rot = r->rot; a.amplitude = r->amplitude; a.freqs = freqs;
+        if (q) {
+            if ((st = check_strides(p->q_stride, p->D, eb)) || (st = check_strides(p->o_stride, p->D, eb))) return st;
+            if (!aligned(q, 16) || !aligned(q_out, 16)) return TLIN_ERR_INVALID_ARG;
+            resolve(p->q_stride, rows, p->D, s1);
+            resolve(p->o_stride, rows, p->D, s2);
+            if (q == q_out && (s1[0] != s2[0] || s1[1] != s2[1])) return TLIN_ERR_INVALID_ARG;
+            a.q = {q, q_out, s1[0], s1[1], s2[0], s2[1], p->H};
+        }
+    } else if (q) {
+        return TLIN_ERR_INVALID_ARG;
+    }
+    resolve(p->k_stride, rows, p->D, s1);
+    resolve(p->kp_stride, page, p->D, s3);
+    a.k = {k, k_pages, s1[0], s1[1], s3[1], 0, p->HK};
+    a.kp_sp = s3[0]; a.kp_sr = s3[2];
+    resolve(p->v_stride, rows, p->D, s1);
+    resolve(p->vp_stride, page, p->D, s3);
+    a.v = {v, v_pages, s1[0], s1[1], s3[1], 0, p->HK};
+    a.vp_sp = s3[0]; a.vp_sr = s3[2];
+    a.table = table; a.lens = lens; a.starts = starts;
+    a.S = p->S; a.M = p->table_width; a.P = p->num_pages; a.lr = log2_of(p->page_rows);
+    a.table_stride = p->table_stride ? p->table_stride : p->table_width;
+    a.tokens = p->T;
+    a.vlanes = power_of_two(row_elements(p->D, eb) * eb / 16);
+    const int E = rope_elements(a.rot, inter, eb);
+    rope_shape(a, E, inter, (q ? p->H : 0) + 2 * p->HK);
+    return launch_rope<true>(a, p->dtype, E, inter, (hipStream_t)stream);
+}
+
+size_t tlin_paged_workspace_bytes(const tlin_paged_params *p)
+{
+    if (check_paged(p)) return 0;
+    PagedWorkspace w;
+    return paged_workspace(paged_shape(p), nullptr, w);
+}
+
+tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const void *k_pages, const void *v_pages,
+                            const int32_t *table, const int32_t *lens, const int32_t *starts, void *O, float *lse, void *ws,
+                            size_t ws_bytes, void *stream)
+{
+    tlin_status st = check_paged(p);
+    if (st) return st;
+    if (!(p->scale > 0.f) || !isfinite(p->scale)) return TLIN_ERR_INVALID_ARG;
+    if ((st = check_strides(p->q_stride, p->D, bytes_of(p->dtype))) || (st = check_strides(p->o_stride, p->D, bytes_of(p->out_dtype)))) return st;
+    if (!q || !k_pages || !v_pages || !table || !lens || !starts || !O) return TLIN_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(O, 16)) return TLIN_ERR_INVALID_ARG;
+    if (!aligned(table, 4) || !aligned(lens, 4) || !aligned(starts, 4) || !aligned(lse, 4)) return TLIN_ERR_INVALID_ARG;
+    if (!ws || !aligned(ws, 256) || ws_bytes < tlin_paged_workspace_bytes(p)) return TLIN_ERR_WORKSPACE;
+    if ((st = check_device())) return st;
+
+    const PagedShape s = paged_shape(p);
+    const bool bf = p->dtype == TLIN_BF16;
+    PagedArgs a = {};
+    PagedWorkspace w;
+    paged_workspace(s, ws, w);
+    int64_t s2[2], s3[3];
+    const int64_t rows[1] = {p->T}, page[2] = {p->HK, p->page_rows};
+    a.Q = q; a.K = k_pages; a.V = v_pages;
+    a.table = table; a.lens = lens; a.starts = starts;
+    a.O = O; a.lse = lse;
+    a.Opart = w.O; a.Mpart = w.M; a.Lpart = w.L;
+    resolve(p->q_stride, rows, p->D, s2);
+    a.q_sh = s2[0]; a.q_sr = s2[1];
+    resolve(p->o_stride, rows, p->D, s2);
+    a.o_sh = s2[0]; a.o_sr = s2[1];
+    resolve(p->kp_stride, page, p->D, s3);
+    a.k_sp = s3[0]; a.k_sh = s3[1]; a.k_sr = s3[2];
+    resolve(p->vp_stride, page, p->D, s3);
+    a.v_sp = s3[0]; a.v_sh = s3[1]; a.v_sr = s3[2];
+    a.S = p->S; a.T = p->T; a.HK = p->HK; a.G = group_of(p);
+    a.D = p->D;
+    a.M = p->table_width; a.P = p->num_pages; a.lr = log2_of(p->page_rows);
+    a.table_stride = p->table_stride ? p->table_stride : p->table_width;
+    a.TB = s.tb;
+    a.shares = s.shares;
+    a.least = 256;
+    a.causal = p->causal != 0;
+    a.out_bf16 = p->out_dtype == TLIN_BF16;
+    a.scale = p->scale;
+    a.c = p->scale * 1.4426950408889634f;
+
+    const hipStream_t hs = (hipStream_t)stream;
+    // Rows that are read once by a call and exceed the last-level cache (256 MB) carry the non-temporal hint, by what the
+    // table and the cache can hold of them.
+    const int64_t named = (int64_t)p->S * p->table_width, most = named < p->num_pages ? named : p->num_pages;
+    const bool nt = p->max_rows <= s.tb && most * p->HK * p->page_rows * p->D * 4 >= (int64_t)192 << 20;
+    const int du = (p->D + 31) / 32 * 32;
+    st = du == 32 ? launch_paged<32>(a, s, bf, nt, hs) : du == 64 ? launch_paged<64>(a, s, bf, nt, hs)
+         : du == 96 ? launch_paged<96>(a, s, bf, nt, hs) : launch_paged<128>(a, s, bf, nt, hs);
+    if (st) return st;
+    // threads to a row's partials: eight where few items are cut into many
+    const int64_t items = (int64_t)p->S * p->HK * ((p->max_rows + s.tb - 1) / s.tb);
+    const bool many = items * 8 <= s.shares;
+    if (!bf) {
+        if (s.dk == 64) return s.nw == 2 ? launch_paged_merge<64, 64, 32>(a, many, hs) : launch_paged_merge<64, 128, 32>(a, many, hs);
+        return s.nw == 2 ? launch_paged_merge<128, 64, 32>(a, many, hs) : launch_paged_merge<128, 128, 32>(a, many, hs);
+    }
+    if (s.dk == 64) return s.nw == 2 ? launch_paged_merge<64, 64, 64>(a, many, hs) : launch_paged_merge<64, 128, 64>(a, many, hs);
+    return s.nw == 2 ? launch_paged_merge<128, 64, 64>(a, many, hs) : s.nw == 4 ? launch_paged_merge<128, 128, 64>(a, many, hs)
+                     : launch_paged_merge<128, 256, 64>(a, many, hs);
+}
+
+tlin_status tlin_pages_free(const tlin_book_params *p, int32_t *table, int32_t *lens, int32_t *refs, const int32_t *seqs,
+                            int32_t n, void *stream)
+{
+    tlin_status st = check_book(p);
+    if (st) return st;
+    if (n < 0 || n > 1 << 24 || !table || !lens || !refs || (n > 0 && !seqs)) return TLIN_ERR_INVALID_ARG;
+    if (n == 0) return TLIN_OK;
+    if ((st = check_device())) return st;
+    BookArgs a = book_args(p);
+    a.table = table; a.lens = lens; a.refs = refs; a.ids = seqs; a.n = n;
+    return launch_kernel((const void *)pages_free_kernel, dim3(n), dim3(256), 0, (hipStream_t)stream, a);
+}
+
+tlin_status tlin_pages_fork(const tlin_book_params *p, int32_t *table, int32_t *lens, int32_t *refs,
+                            const int32_t *parents, const int32_t *children, int32_t n, int32_t *status, void *stream)
+{
+    tlin_status st = check_book(p);
+    if (st) return st;
+    if (n < 0 || n > 1 << 24 || !table || !lens || !refs || (n > 0 && (!parents || !children || !status))) return TLIN_ERR_INVALID_ARG;
+    if (n == 0) return TLIN_OK;
+    if ((st = check_device())) return st;
+    BookArgs a = book_args(p);
+    a.table = table; a.lens = lens; a.refs = refs; a.ids = parents; a.children = children; a.n = n; a.status = status;
+    return launch_kernel((const void *)pages_fork_kernel, dim3(n), dim3(256), 0, (hipStream_t)stream, a);
+}
+
+// reserve: first and nth_copy [S], fresh [P].  compact: live pages of every block, rank [P], L.
+size_t tlin_pages_workspace_bytes(const tlin_book_params *p)
+{
+    if (check_book(p)) return 0;
+    const size_t reserve = 2 * (size_t)p->S + p->num_pages, compact = (size_t)page_blocks(p) + p->num_pages + 1;
+    return 4 * (reserve > compact ? reserve : compact);
+}
+
+tlin_status tlin_pages_reserve(const tlin_book_params *p, int32_t *table, int32_t *lens, int32_t *refs, const int32_t *want,
+                               int32_t *moves, int32_t *count, int32_t *status, void *ws, size_t ws_bytes, void *stream)
+{
+    tlin_status st = check_book(p);
+    if (st) return st;
+    if (!table || !lens || !refs || !want || !moves || !count || !status) return TLIN_ERR_INVALID_ARG;
+    if (!ws || !aligned(ws, 256) || ws_bytes < tlin_pages_workspace_bytes(p)) return TLIN_ERR_WORKSPACE;
+    if ((st = check_device())) return st;
+    BookArgs a = book_args(p);
+    a.table = table; a.lens = lens; a.refs = refs; a.ids = want; a.moves = moves; a.count = count; a.status = status;
+    a.scratch = (int32_t *)ws;
+    return launch_kernel((const void *)pages_reserve_kernel, dim3(1), dim3(1024), 0, (hipStream_t)stream, a);
+}
+
+tlin_status tlin_pages_compact(const tlin_book_params *p, const int32_t *table, const int32_t *refs, int32_t *table_out,
+                               int32_t *refs_out, int32_t *moves, int32_t *count, void *ws, size_t ws_bytes, void *stream)
+{
+    tlin_status st = check_book(p);
+    if (st) return st;
+    if (!table || !refs || !table_out || !refs_out || (!moves && p->num_pages > 1) || !count) return TLIN_ERR_INVALID_ARG;
+    if (!ws || !aligned(ws, 256) || ws_bytes < tlin_pages_workspace_bytes(p)) return TLIN_ERR_WORKSPACE;
+    if ((st = check_device())) return st;
+    BookArgs a = book_args(p);
+    a.table_in = table; a.refs_in = refs; a.table = table_out; a.refs = refs_out; a.moves = moves; a.count = count;
+    a.scratch = (int32_t *)ws;
+    a.nblocks = page_blocks(p);
+    const hipStream_t hs = (hipStream_t)stream;
+    if ((st = launch_kernel((const void *)pages_count_kernel, dim3(a.nblocks), dim3(1024), 0, hs, a))) return st;
+    if ((st = launch_kernel((const void *)pages_plan_kernel, dim3(a.nblocks), dim3(1024), 0, hs, a))) return st;
+    const int64_t entries = (int64_t)p->S * p->table_width > p->num_pages ? (int64_t)p->S * p->table_width : p->num_pages;
+    const int64_t blocks = (entries + 255) / 256;
+    return launch_kernel((const void *)pages_apply_kernel, dim3((unsigned)(blocks < 8 * kNumCU ? blocks : 8 * kNumCU)), dim3(256), 0, hs, a);
+}
+
+tlin_status tlin_pages_copy(const tlin_cache_params *p, void *a, void *b, const int32_t *moves, const int32_t *count,
+                            int32_t max_moves, void *stream)
+{
+    if (!p || p->layers < 1 || p->num_pages < 1 || p->num_pages > kMaxRows || p->HK < 1 || p->HK > 1 << 20 || !is_type(p->dtype)) return TLIN_ERR_INVALID_ARG;
+    if (!good_dim(p->D) || !good_page_rows(p->page_rows)) return TLIN_ERR_UNSUPPORTED;
+    const int eb = bytes_of(p->dtype);
+    tlin_status st;
+    if ((st = check_strides(p->a_stride, p->D, eb))) return st;
+    if (b && (st = check_strides(p->b_stride, p->D, eb))) return st;
+    if (!a || !aligned(a, 16) || !aligned(b, 16) || max_moves < 0 || (max_moves > 0 && !moves)) return TLIN_ERR_INVALID_ARG;
+    for (int c = 0; c < (b ? 2 : 1); ++c)
+        if (p->layer_stride[c] < 0 || p->layer_stride[c] % (16 / eb)) return TLIN_ERR_INVALID_ARG;
+    if (max_moves == 0) return TLIN_OK;
+    if ((st = check_device())) return st;
+    CopyArgs g = {};
+    g.moves = moves; g.count = count; g.max_moves = max_moves; g.P = p->num_pages;
+    g.layers = p->layers; g.HK = p->HK; g.R = p->page_rows;
+    g.caches = b ? 2 : 1;
+    const int re = row_elements(p->D, eb);
+    g.row_pieces = re * eb / 16;
+    g.pieces = (int64_t)p->HK * p->page_rows * g.row_pieces;
+    const int64_t sizes[2] = {p->HK, p->page_rows};
+    for (int c = 0; c < g.caches; ++c) {
+        int64_t s[3];
+        if (c == 0) resolve(p->a_stride, sizes, p->D, s);
+        else resolve(p->b_stride, sizes, p->D, s);
+        g.cache[c] = (char *)(c == 0 ? a : b);
+        g.layer[c] = (p->layer_stride[c] ? p->layer_stride[c] : s[0] * p->num_pages) * eb;
+        g.page[c] = s[0] * eb; g.head[c] = s[1] * eb; g.row[c] = s[2] * eb;
+        // heads outside rows or rows outside heads, without gaps
+        g.flat[c] = (s[2] == re && s[1] == (int64_t)re * p->page_rows) || (s[1] == re && s[2] == (int64_t)re * p->HK) || (p->HK == 1 && s[2] == re);
+    }
+    // 16 KB to a work item: four pieces a thread
+    g.parts = (int)((g.pieces + 1023) / 1024);
+    const int64_t most = (int64_t)max_moves * g.layers * g.caches * g.parts;
+    return launch_kernel((const void *)pages_copy_kernel, dim3((unsigned)(most < 8 * kNumCU ? most : 8 * kNumCU)), dim3(256), 0, (hipStream_t)stream, g);
+}
+
+}  // extern "C"
