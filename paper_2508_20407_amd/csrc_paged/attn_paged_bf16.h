@@ -37,8 +37,9 @@ struct PagedBf16 {
 };
 
 template <int DU, int NW, bool NT>
-__device__ __forceinline__ void paged_bf16_item(const PagedArgs &a, const Place &p, int t0, int t1, bool direct, int64_t slot)
+__device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, bool direct, int64_t slot)
 {
+    ConstPagedArgs &a = *args_again();
     using C = PagedBf16<DU, NW, NT>;
     constexpr int DK = C::DK, BN = C::BN, BM = C::BM, ROWB = C::ROWB, TILE_B = C::TILE_B, CPR = C::CPR, RPI = C::RPI;
     constexpr int NDMA = C::NDMA, DS = C::DS, DB = C::DB, NGW = C::NGW;
@@ -378,31 +379,32 @@ __device__ __forceinline__ void paged_bf16_item(const PagedArgs &a, const Place 
 
     // ---- output.  Accumulator register v of block db is column 32 db + 8 (v / 4) + 4 h + v % 4.
     const float lt = xhalf_sum(l);
+    ConstPagedArgs &z = *args_again();
     if (mine) {
         if (direct) {
             const float inv = lt > 0.f ? 1.0f / lt : lt == 0.f ? 0.f : lt;      // a row that sees nothing: zeros
-            const int64_t off = hd * a.o_sh + qrow * a.o_sr;
+            const int64_t off = hd * z.o_sh + qrow * z.o_sr;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int d = 32 * db + 8 * g + 4 * h;
-                    if (d >= a.D) continue;
+                    if (d >= z.D) continue;
                     f32x4 o;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[e] = oacc[db][4 * g + e] * inv;
-                    if (a.out_bf16) {
+                    if (z.out_bf16) {
                         bf16x4 ob;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) ob[e] = (__bf16)o[e];
-                        *(bf16x4 *)((__bf16 *)a.O + off + d) = ob;
+                        *(bf16x4 *)((__bf16 *)z.O + off + d) = ob;
                     } else {
-                        *(f32x4 *)((float *)a.O + off + d) = o;
+                        *(f32x4 *)((float *)z.O + off + d) = o;
                     }
                 }
-            if (a.lse && h == 0) a.lse[(int64_t)hd * a.T + qrow] = m * a.scale + logf(lt);
+            if (z.lse && h == 0) z.lse[(int64_t)hd * z.T + qrow] = m * z.scale + logf(lt);
         } else {
-            float *op = a.Opart + (slot * BM + r) * DK;
+            float *op = z.Opart + (slot * BM + r) * DK;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -413,8 +415,8 @@ __device__ __forceinline__ void paged_bf16_item(const PagedArgs &a, const Place 
                     *(f32x4 *)(op + 32 * db + 8 * g + 4 * h) = o;
                 }
             if (h == 0) {
-                a.Mpart[slot * BM + r] = m * a.c;
-                a.Lpart[slot * BM + r] = lt;
+                z.Mpart[slot * BM + r] = m * z.c;
+                z.Lpart[slot * BM + r] = lt;
             }
         }
     }
@@ -425,22 +427,13 @@ __device__ __forceinline__ void paged_bf16_item(const PagedArgs &a, const Place 
 
 template <int DU, int NW, bool NT>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW < 8 ? 2 : 1, 8)))
-void paged_bf16_kernel(const PagedArgs a)
+void paged_bf16_kernel(const PagedArgs)
 {
     using C = PagedBf16<DU, NW, NT>;
     __shared__ PlaceLds lds;
-    Place p;
-    const int w = xcd_remap(blockIdx.x, gridDim.x);
-    if (!find_place<NW * 64>(a, w, p, lds)) return;
-    int64_t left = min(p.quota, p.total - w * p.quota);
-    for (;;) {
-        const int64_t n = block_rows(a, p.q, p.qb), x1 = min(n, p.x + left);
-        const int t0 = tiles_to<C::BN>(p.x), t1 = tiles_to<C::BN>(x1), nt = tiles_to<C::BN>(n);
-        if (t0 < t1) paged_bf16_item<DU, NW, NT>(a, p, t0, t1, t0 == 0 && t1 == nt, 2 * (int64_t)w + (p.x > 0 ? 0 : 1));
-        left -= x1 - p.x;
-        if (left <= 0) return;
-        next_item(a, p);
-    }
+    share_items<NW * 64, C::BN>(xcd_remap(blockIdx.x, gridDim.x), lds, [](const Place &p, int t0, int t1, bool whole, int64_t slot) __attribute__((always_inline)) {
+        paged_bf16_item<DU, NW, NT>(p, t0, t1, whole, slot);
+    });
 }
 
 }  // namespace tlin

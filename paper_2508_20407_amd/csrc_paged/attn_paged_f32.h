@@ -31,8 +31,9 @@ struct PagedF32 {
 };
 
 template <int DU, int NW>
-__device__ __forceinline__ void paged_f32_item(const PagedArgs &a, const Place &p, int t0, int t1, bool direct, int64_t slot)
+__device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, bool direct, int64_t slot)
 {
+    ConstPagedArgs &a = *args_again();
     using C = PagedF32<DU, NW>;
     constexpr int DK = C::DK, BN = C::BN, BM = C::BM, ROWB = C::ROWB, TILE_B = C::TILE_B, CPR = C::CPR, RPI = C::RPI;
     constexpr int NDMA = C::NDMA, NGW = C::NGW;
@@ -197,10 +198,11 @@ __device__ __forceinline__ void paged_f32_item(const PagedArgs &a, const Place &
     }
 
     const float lt = xhalf_sum(l);
+    ConstPagedArgs &z = *args_again();
     if (mine) {
         const float inv = !direct ? 1.f : lt > 0.f ? 1.0f / lt : lt == 0.f ? 0.f : lt;
-        const int64_t off = hd * a.o_sh + qrow * a.o_sr;
-        float *op = a.Opart + (slot * BM + r) * DK;
+        const int64_t off = hd * z.o_sh + qrow * z.o_sr;
+        float *op = z.Opart + (slot * BM + r) * DK;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -211,23 +213,23 @@ __device__ __forceinline__ void paged_f32_item(const PagedArgs &a, const Place &
                 for (int e = 0; e < 4; ++e) o[e] = oacc[db][4 * g + e] * inv;
                 if (!direct) {
                     *(f32x4 *)(op + d) = o;
-                } else if (d < a.D) {
-                    if (a.out_bf16) {
+                } else if (d < z.D) {
+                    if (z.out_bf16) {
                         bf16x4 ob;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) ob[e] = (__bf16)o[e];
-                        *(bf16x4 *)((__bf16 *)a.O + off + d) = ob;
+                        *(bf16x4 *)((__bf16 *)z.O + off + d) = ob;
                     } else {
-                        *(f32x4 *)((float *)a.O + off + d) = o;
+                        *(f32x4 *)((float *)z.O + off + d) = o;
                     }
                 }
             }
         if (h == 0) {
             if (!direct) {
-                a.Mpart[slot * BM + r] = m * a.c;
-                a.Lpart[slot * BM + r] = lt;
-            } else if (a.lse) {
-                a.lse[(int64_t)hd * a.T + qrow] = m * a.scale + logf(lt);
+                z.Mpart[slot * BM + r] = m * z.c;
+                z.Lpart[slot * BM + r] = lt;
+            } else if (z.lse) {
+                z.lse[(int64_t)hd * z.T + qrow] = m * z.scale + logf(lt);
             }
         }
     }
@@ -237,22 +239,13 @@ __device__ __forceinline__ void paged_f32_item(const PagedArgs &a, const Place &
 
 template <int DU, int NW>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 8)))
-void paged_f32_kernel(const PagedArgs a)
+void paged_f32_kernel(const PagedArgs)
 {
     using C = PagedF32<DU, NW>;
     __shared__ PlaceLds lds;
-    Place p;
-    const int w = xcd_remap(blockIdx.x, gridDim.x);
-    if (!find_place<NW * 64>(a, w, p, lds)) return;
-    int64_t left = min(p.quota, p.total - w * p.quota);
-    for (;;) {
-        const int64_t n = block_rows(a, p.q, p.qb), x1 = min(n, p.x + left);
-        const int t0 = tiles_to<C::BN>(p.x), t1 = tiles_to<C::BN>(x1), nt = tiles_to<C::BN>(n);
-        if (t0 < t1) paged_f32_item<DU, NW>(a, p, t0, t1, t0 == 0 && t1 == nt, 2 * (int64_t)w + (p.x > 0 ? 0 : 1));
-        left -= x1 - p.x;
-        if (left <= 0) return;
-        next_item(a, p);
-    }
+    share_items<NW * 64, C::BN>(xcd_remap(blockIdx.x, gridDim.x), lds, [](const Place &p, int t0, int t1, bool whole, int64_t slot) __attribute__((always_inline)) {
+        paged_f32_item<DU, NW>(p, t0, t1, whole, slot);
+    });
 }
 
 }  // namespace tlin

@@ -1,9 +1,9 @@
 // Joins the partials of the items that a cut between two shares goes through.
 //
 // A partial of a row is (O, m, l): O = sum_j 2^(x_j - m) V_j, l = sum_j 2^(x_j - m) over its keys, x_j the logit in base-2
-// units.  Over the union of the partials O = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s, M the largest m_s.  A
-// workgroup looks at one cut: if its item begins in the share before the cut, the workgroup joins the item's partials
-// (a later cut through the same item has nothing to do).  No atomics: results do not depend on who comes first.
+// units.  Over the union of the partials O = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s, M the largest m_s.  The
+// workgroups of a share join the item that begins in it and ends in a later one, if there is one.  No atomics: results do
+// not depend on who comes first.
 #pragma once
 #include "share.h"
 
@@ -12,30 +12,18 @@ namespace tlin {
 constexpr int kMergeThreads = 256;
 
 // LN threads share a (row, 4 columns): each takes every LN-th partial.  ROWS rows of the block at blockIdx.y.
-template <int DK, int BM, int BN, int LN>
+// LN threads share a (row, 4 columns): each takes every LN-th partial.  blockIdx.y: which of the item's rows.
+template <int DK, int LN>
 __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedArgs a)
 {
     constexpr int TPR = DK / 4;                         // threads across a row
     constexpr int RPB = kMergeThreads / (TPR * LN);     // rows at a time
-    __shared__ PlaceLds lds;
     __shared__ float red[LN > 1 ? kMergeThreads * 6 : 1];
-    Place p;
-    const int w = blockIdx.x + 1;                       // the cut before share w
-    if (!find_place<kMergeThreads>(a, w, p, lds)) return;
-    if (p.x == 0 || p.x > p.quota) return;              // no item goes across, or it began before the share in front
-    const int64_t n = block_rows(a, p.q, p.qb), start = (int64_t)w * p.quota - p.x;
-    const int64_t first = p.x;                          // length of the item's part in share w - 1
-    const int nt = tiles_to<BN>(n);
-    const int tile1 = tiles_to<BN>(first);
-    if (tile1 >= nt) return;                            // share w - 1 held all of its tiles and wrote the result
-    const int last = (int)((start + n - 1) / p.quota);  // last share with a part of the item
-    // share w holds all tiles: written there
-    if (tile1 == 0 && (last == w || tiles_to<BN>(first + p.quota) >= nt)) return;
-
-    const int rows = min(a.TB, p.q.W - p.qb * a.TB) * a.G;
+    const int w = blockIdx.x;
+    const CutItem cut = a.cuts[w];
+    const int rows = cut.rows, BM = a.BM;
     const int cg = threadIdx.x % TPR, ln = threadIdx.x / TPR % LN, rb = threadIdx.x / (TPR * LN);
     const int c4 = 4 * cg;
-    const int parts = last - w + 2;
     for (int r0 = blockIdx.y * RPB; r0 < rows; r0 += gridDim.y * RPB) {
         const int r = r0 + rb;
         const bool live = r < rows;
@@ -43,7 +31,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedA
         f32x4 num = {0.f, 0.f, 0.f, 0.f};
         constexpr int NB = 4;
         if (live)
-            for (int k0 = ln; k0 < parts; k0 += NB * LN) {
+            for (int k0 = cut.part0 + ln; k0 < cut.part1; k0 += NB * LN) {
                 float ms[NB], ls[NB];
                 f32x4 os[NB];
 #pragma unroll
@@ -52,11 +40,8 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedA
                     ls[e] = 0.f;
                     os[e] = f32x4{0.f, 0.f, 0.f, 0.f};
                     const int k = k0 + e * LN;
-                    if (k >= parts) continue;
-                    // tiles of part k: an empty part has no partial
-                    const int64_t x0 = k == 0 ? 0 : first + (k - 1) * p.quota, x1 = min(first + k * p.quota, n);
-                    if (tiles_to<BN>(x0) >= tiles_to<BN>(x1)) continue;
-                    const int64_t slot = k == 0 ? 2 * (int64_t)(w - 1) + 1 : 2 * (int64_t)(w - 1 + k);
+                    if (k >= cut.part1) continue;
+                    const int64_t slot = 2 * (int64_t)(w + k) + (k == 0);
                     const int64_t idx = slot * BM + r;
                     ms[e] = a.Mpart[idx];
                     ls[e] = a.Lpart[idx];
@@ -93,8 +78,8 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedA
             }
         }
         if (!live || c4 >= a.D) continue;
-        const int tok = r / a.G, hd = p.head * a.G + r - tok * a.G;
-        const int64_t row = p.q.first + p.qb * a.TB + tok;
+        const int tok = r / a.G, hd = cut.head + r - tok * a.G;
+        const int64_t row = cut.row + tok;
         const f32x4 o = num * (den > 0.f ? 1.0f / den : den == 0.f ? 0.f : den);      // (not a number stays that)
         const int64_t off = hd * a.o_sh + row * a.o_sr + c4;
         if (a.out_bf16) {

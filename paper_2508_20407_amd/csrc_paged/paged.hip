@@ -125,14 +125,15 @@ PagedShape paged_shape(const tlin_paged_params *p)
     return s;
 }
 
-struct PagedWorkspace { float *O, *M, *L; };
+struct PagedWorkspace { float *O, *M, *L; CutItem *cuts; };
 size_t paged_workspace(const PagedShape &s, void *ws, PagedWorkspace &w)
 {
     const size_t rows = 2 * (size_t)s.shares * s.bm();
     w.O = (float *)ws;
     w.M = w.O + rows * s.dk;
     w.L = w.M + rows;
-    return (rows * s.dk + 2 * rows) * sizeof(float);
+    w.cuts = (CutItem *)(w.L + rows);
+    return (rows * s.dk + 2 * rows) * sizeof(float) + s.shares * sizeof(CutItem);
 }
 
 template <int DU, int NW, bool NT>
@@ -163,14 +164,16 @@ tlin_status launch_paged(const PagedArgs &a, const PagedShape &s, bool bf, bool 
     return TLIN_ERR_UNSUPPORTED;      // (not reached: eight waves are for rows of 128)
 }
 
-template <int DK, int BM, int BN>
-tlin_status launch_paged_merge(const PagedArgs &a, bool many, hipStream_t st)
+// Threads to a row's partials: eight where there are too few rows to fill the chip with one.
+template <int DK>
+tlin_status launch_paged_merge(const PagedArgs &a, int64_t items, hipStream_t st)
 {
-    const void *kernel = many ? (const void *)paged_merge_kernel<DK, BM, BN, 8> : (const void *)paged_merge_kernel<DK, BM, BN, 1>;
-    const int rpb = kMergeThreads / (DK / 4) / (many ? 8 : 1);
     const int rows = a.TB * a.G;
+    const bool many = items * rows * (DK / 4) < kNumCU * 512;
+    const void *kernel = many ? (const void *)paged_merge_kernel<DK, 8> : (const void *)paged_merge_kernel<DK, 1>;
+    const int rpb = kMergeThreads / (DK / 4) / (many ? 8 : 1);
     int blocks = (rows + rpb - 1) / rpb;
-    if (blocks > 8) blocks = 8;
+    if (blocks > 16) blocks = 16;
     return launch_kernel(kernel, dim3(a.shares - 1, blocks), dim3(kMergeThreads), 0, st, a);
 }
 
@@ -318,7 +321,7 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
     a.Q = q; a.K = k_pages; a.V = v_pages;
     a.table = table; a.lens = lens; a.starts = starts;
     a.O = O; a.lse = lse;
-    a.Opart = w.O; a.Mpart = w.M; a.Lpart = w.L;
+    a.Opart = w.O; a.Mpart = w.M; a.Lpart = w.L; a.cuts = w.cuts;
     resolve(p->q_stride, rows, p->D, s2);
     a.q_sh = s2[0]; a.q_sr = s2[1];
     resolve(p->o_stride, rows, p->D, s2);
@@ -331,7 +334,7 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
     a.D = p->D;
     a.M = p->table_width; a.P = p->num_pages; a.lr = log2_of(p->page_rows);
     a.table_stride = p->table_stride ? p->table_stride : p->table_width;
-    a.TB = s.tb;
+    a.TB = s.tb; a.BM = s.bm();
     a.shares = s.shares;
     a.least = 256;
     a.causal = p->causal != 0;
@@ -348,16 +351,8 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
     st = du == 32 ? launch_paged<32>(a, s, bf, nt, hs) : du == 64 ? launch_paged<64>(a, s, bf, nt, hs)
          : du == 96 ? launch_paged<96>(a, s, bf, nt, hs) : launch_paged<128>(a, s, bf, nt, hs);
     if (st) return st;
-    // threads to a row's partials: eight where few items are cut into many
     const int64_t items = (int64_t)p->S * p->HK * ((p->max_rows + s.tb - 1) / s.tb);
-    const bool many = items * 8 <= s.shares;
-    if (!bf) {
-        if (s.dk == 64) return s.nw == 2 ? launch_paged_merge<64, 64, 32>(a, many, hs) : launch_paged_merge<64, 128, 32>(a, many, hs);
-        return s.nw == 2 ? launch_paged_merge<128, 64, 32>(a, many, hs) : launch_paged_merge<128, 128, 32>(a, many, hs);
-    }
-    if (s.dk == 64) return s.nw == 2 ? launch_paged_merge<64, 64, 64>(a, many, hs) : launch_paged_merge<64, 128, 64>(a, many, hs);
-    return s.nw == 2 ? launch_paged_merge<128, 64, 64>(a, many, hs) : s.nw == 4 ? launch_paged_merge<128, 128, 64>(a, many, hs)
-                     : launch_paged_merge<128, 256, 64>(a, many, hs);
+    return s.dk == 64 ? launch_paged_merge<64>(a, items, hs) : launch_paged_merge<128>(a, items, hs);
 }
 
 tlin_status tlin_pages_free(const tlin_book_params *p, int32_t *table, int32_t *lens, int32_t *refs, const int32_t *seqs,
