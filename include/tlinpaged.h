@@ -79,7 +79,7 @@ typedef struct {
     float scale;          /* logit multiplier, finite and > 0 */
     int32_t table_stride; /* elements from one sequence's table row to the next; 0 = table_width */
     /* {head, row} of [heads, T, D] tensors, {page, head, row} of the caches [num_pages, HK, page_rows, D]; all 0 =
-     * dense.  Row strides below 32 MiB. */
+     * dense.  Row strides below 32 MiB; a cache's page stride, and page_rows row strides, below 4 GiB. */
     int64_t q_stride[2], o_stride[2], k_stride[2], v_stride[2], kp_stride[3], vp_stride[3];
 } tlin_paged_params;
 

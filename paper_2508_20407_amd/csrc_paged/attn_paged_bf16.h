@@ -10,7 +10,7 @@
 // What paging changes:
 //   - Rows come from pages of 16 or more rows, so a tile is four groups of 16 rows that lie anywhere.  A direct load covers 4
 //     or 8 rows, never two groups: it takes its group's page through a buffer descriptor of its own, whose size ends
-//     with the sequence (what a page holds behind it, NaNs perhaps, arrives as zeros).  Page ids are read three tiles
+//     with the sequence (what a page holds behind it, NaNs perhaps, arrives as zeros).  Page ids are read four tiles
 //     ahead, by lanes 0 to 3, with an ordinary load whose arrival the tile's own wait covers: a scalar load would make the
 //     LDS reads of a whole phase wait for it (both count on lgkmcnt and scalar loads return out of order).
 //   - The 32 query columns of a wave are (new row, query head) pairs that share a key head, rows outside: the cache is read
@@ -21,6 +21,18 @@
 #include "share.h"
 
 namespace tlin {
+
+constexpr int SG_SALU = 0x004;       // sched_group_barrier mask (the others: attn_bf16_pipe.h)
+
+// The lane, computed again from here on.
+__device__ __forceinline__ int lane_again()
+{
+    int ones = -1;
+    asm volatile("" : "+v"(ones));
+    return __builtin_amdgcn_mbcnt_hi(ones, __builtin_amdgcn_mbcnt_lo(ones, 0));
+}
+// A (new row, query head) pair of a block: the pair, whether there is one, its row and head, the last key it sees.
+struct QueryRow { int r; bool mine; int64_t row; int head, lim; };
 
 // DU: columns computed, at least a.D (32, 64: rows of 64 elements in LDS; 96, 128: of 128).  NT: non-temporal tile loads.
 template <int DU, int NW, bool NT>
@@ -59,21 +71,26 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
         const int key = (t0 + min(n, nt - 1)) * BN + 16 * (lane & 3);
         return row[min(key >> a.lr, a.M - 1)];
     };
-    // idA of tile n + 1, idB of tile n + 2, idC of tile n + 3 (on its way) during step n
-    const int id0 = load_ids(0);
-    int idA = 0, idB = load_ids(1), idC = load_ids(2);
+    const int id0 = load_ids(0), id1 = load_ids(1);
+    int idB = load_ids(2), idC = load_ids(3);      // of tiles n + 2 and n + 3 during step n (the latter on its way until its top)
 
-    // ---- this lane's query row
+    // ---- this lane's query row: (new row, query head) pair r of the block.  Computed where it is needed, for the queries, a
+    // mask and the output, and not kept through the loop, whose registers are all taken.
     const int tok0 = p.qb * a.TB;                              // first new row of the block
     const int ntok = min(a.TB, p.q.W - tok0);
-    const int r = wave * 32 + j;
-    const int tok = r / a.G, hq = r - tok * a.G;
-    const bool mine = tok < ntok;
-    const int64_t qrow = p.q.first + tok0 + (mine ? tok : 0);
-    const int hd = p.head * a.G + (mine ? hq : 0);
-    const int lim = a.causal ? min(len - 1, ctx + tok0 + tok) : len - 1;       // last key this row sees
+    const int first = p.q.first, head = p.head;
+    auto query_row = [=](const auto &b) __attribute__((always_inline)) {
+        QueryRow x;
+        x.r = wave * 32 + (lane_again() & 31);
+        const int G = b.G, tok = (int)(((float)x.r + 0.5f) * b.per_G), hq = x.r - tok * G;
+        x.mine = tok < ntok;
+        x.row = first + tok0 + (x.mine ? tok : 0);
+        x.head = head * G + (x.mine ? hq : 0);
+        x.lim = b.causal ? min(len - 1, ctx + tok0 + tok) : len - 1;
+        return x;
+    };
     // of the wave: first and last limit of its rows; the last tile it computes on, or -1
-    const int wt0 = wave * 32 / a.G, wt1 = min((wave * 32 + 31) / a.G, ntok - 1);
+    const int wt0 = (int)((wave * 32 + 0.5f) * a.per_G), wt1 = min((int)((wave * 32 + 31.5f) * a.per_G), ntok - 1);
     const int lim0 = uniform(a.causal ? min(len - 1, ctx + tok0 + wt0) : len - 1);
     const int lim1 = uniform(a.causal ? min(len - 1, ctx + tok0 + wt1) : len - 1);
     const int tl = uniform(wt0 >= ntok || lim1 < 0 ? -1 : min(lim1 / BN - t0, nt - 1));
@@ -81,7 +98,8 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
     const int dchunks = (a.D + 7) >> 3;
     bf16x8 qf[DS];
     {
-        const __bf16 *qp = (const __bf16 *)a.Q + hd * a.q_sh + qrow * a.q_sr + 8 * h;
+        const QueryRow x = query_row(a);
+        const __bf16 *qp = (const __bf16 *)a.Q + x.head * a.q_sh + x.row * a.q_sr + 8 * h;
 #pragma unroll
         for (int s = 0; s < DS; ++s) {
             const int keep = a.D - 16 * s - 8 * h;             // columns of this fragment that exist
@@ -90,21 +108,18 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
             if (keep < 8) u[2] = u[3] = 0;                     // (D is a multiple of 4)
             qf[s] = __builtin_bit_cast(bf16x8, u);
         }
-        // used here, so that the wait for these loads sits before the tile loop
-#pragma unroll
-        for (int s = 0; s < DS; ++s) asm volatile("" : "+v"(qf[s]));
     }
 
     // ---- tile loads.  Load i of this wave covers tile rows (wave * NDMA + i) * RPI ..; this lane lands on row drow, chunk
     // position lane % CPR, and fetches chunk (lane % CPR) ^ swz(row); offsets count from the row's group of 16
-    const int64_t k_rb = a.k_sr * 2, v_rb = a.v_sr * 2;
+    const unsigned k_rb = (unsigned)a.k_sr * 2, v_rb = (unsigned)a.v_sr * 2, kp_b = (unsigned)(a.k_sp * 2), vp_b = (unsigned)(a.v_sp * 2);
     unsigned koff[NDMA], voff[NDMA];
 #pragma unroll
     for (int i = 0; i < NDMA; ++i) {
         const int drow = (wave * NDMA + i) * RPI + lane / CPR;
         const int kc = (lane % CPR) ^ Swz<DK>::k(drow), vc = (lane % CPR) ^ Swz<DK>::v(drow);
-        koff[i] = kc >= dchunks ? kNoChunk : (unsigned)((drow & 15) * k_rb) + (kc << 4);
-        voff[i] = vc >= dchunks ? kNoChunk : (unsigned)((drow & 15) * v_rb) + (vc << 4);
+        koff[i] = kc >= dchunks ? kNoChunk : (drow & 15) * k_rb + (kc << 4);
+        voff[i] = vc >= dchunks ? kNoChunk : (drow & 15) * v_rb + (vc << 4);
     }
     const unsigned lds_wave = uniform((int)(lds_offset(Ks) + wave * (NDMA * 1024)));
     const char *const Kg = (const char *)a.K + p.head * a.k_sh * 2;
@@ -114,25 +129,27 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
         const int key = (t0 + min(n, nt - 1)) * BN + 16 * (lane & 3);
         return (unsigned)(__builtin_amdgcn_ballot_w64(key < len && (unsigned)ids >= (unsigned)a.P) & 15);
     };
-    auto descriptor = [&](const char *base, int64_t sp, int64_t rb, int ids, int n, int g) __attribute__((always_inline)) {
+    // Of the 16 rows of group g of local tile n: page and row in 32-bit bytes (the host bounds the strides), as many
+    // bytes as there are rows below the sequence's end, none where the page is missing.
+    auto descriptor = [&](const char *base, unsigned page_bytes, unsigned rb, int ids, int n, int g) __attribute__((always_inline)) {
         const int key = (t0 + min(n, nt - 1)) * BN + 16 * g;
-        const int id = __builtin_amdgcn_readlane(ids, g);
-        const bool there = (unsigned)id < (unsigned)a.P;
-        const int rows = there ? max(min(16, len - key), 0) : 0;
-        return tile_descriptor(base + (there ? id : 0) * (sp * 2) + (key & ((1 << a.lr) - 1)) * rb, (unsigned)(rows * rb));
+        const unsigned id = __builtin_amdgcn_readlane(ids, g);
+        const bool there = id < (unsigned)a.P;
+        const unsigned rows = there ? max(min(16, len - key), 0) : 0;
+        return tile_descriptor(base + (uint64_t)(there ? id : 0) * page_bytes + (key & ((1 << a.lr) - 1)) * rb, rows * rb);
     };
     const int g0 = wave * NDMA * RPI / 16;                     // first group of this wave
     struct Desc { u32x4 d[NGW]; };
     auto descriptors_k = [&](int ids, int n) __attribute__((always_inline)) {
         Desc x;
 #pragma unroll
-        for (int g = 0; g < NGW; ++g) x.d[g] = descriptor(Kg, a.k_sp, k_rb, ids, n, g0 + g);
+        for (int g = 0; g < NGW; ++g) x.d[g] = descriptor(Kg, kp_b, k_rb, ids, n, g0 + g);
         return x;
     };
     auto descriptors_v = [&](int ids, int n) __attribute__((always_inline)) {
         Desc x;
 #pragma unroll
-        for (int g = 0; g < NGW; ++g) x.d[g] = descriptor(Vg, a.v_sp, v_rb, ids, n, g0 + g);
+        for (int g = 0; g < NGW; ++g) x.d[g] = descriptor(Vg, vp_b, v_rb, ids, n, g0 + g);
         return x;
     };
     auto dma_k = [&](const Desc &x, int i, int stage) __attribute__((always_inline)) {
@@ -210,6 +227,7 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
     };
     // keys behind this row's limit, and keys of missing pages
     auto mask = [&](f32x16 (&S)[2], int key0, unsigned miss) __attribute__((always_inline)) {
+        const int lim = query_row(*args_again()).lim, h = lane_again() >> 5;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -241,21 +259,22 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
         }
     };
 
+    // during step n: K(n + 2), V(n + 1), groups of tile n + 1 that are missing
     Desc dk, dv;
-    unsigned miss = missing(id0, 0);       // of tile n + 1 during step n; of tile 0 before
-    // the top of step n: this wave's loads have landed and every wave has left the stages they will be followed in by
-    // K(n + 2), V(n + 1)
+    unsigned miss;
+    // The top of step n: this wave's loads have landed, and every wave has left the stages that K(n + 2) and V(n + 1) go to.
     auto top = [&](int n, int kst) __attribute__((always_inline)) {
         wait_vmcnt<0>();
         asm volatile("" : "+v"(idC));
         scrub(kst);
         __builtin_amdgcn_s_barrier();
-        idA = idB;
+    };
+    // what step n + 1 loads; the ids of tile n + 4 set out
+    auto advance = [&](int n) __attribute__((always_inline)) {
+        dk = descriptors_k(idC, n + 3);
+        dv = descriptors_v(idB, n + 2);
+        miss = missing(idB, n + 2);
         idB = idC;
-        idC = load_ids(n + 3);
-        dk = descriptors_k(idB, n + 2);
-        dv = descriptors_v(idA, n + 1);
-        miss = missing(idA, n + 1);
     };
 
     constexpr int KPF = 4, VPF = 2, WA = 2;     // reads ahead of K and V operands, quarters of the weights in phase A
@@ -290,6 +309,7 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
         });
         __builtin_amdgcn_sched_barrier(0);
         if ((t0 + n + 2) * BN - 1 > lim0 || miss) mask(Sn, (t0 + n + 1) * BN, miss);
+        const int idN = load_ids(n + 4);
         // phase B: value products of tile n, the rest of its weights, the row maximum of tile n + 1
 #pragma unroll
         for (int i = 0; i < 2 * DB; ++i) pv_op(i, v_read(i, VST * TILE_B));
@@ -298,6 +318,11 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
 #pragma unroll
         for (int i = 2 * DB; i < 4 * DB; ++i) pv_op(i, v_read(i, VST * TILE_B));
         const float mx = row_max(Sn);
+        // (some 30 scalar instructions a group: behind the barrier, ahead of the first product, they cost a tenth of the step)
+        advance(n);
+#pragma unroll
+        for (int g = 0; g < NGW; ++g) asm volatile("" : "+s"(dk.d[g]), "+s"(dv.d[g]));
+        asm volatile("" : "+s"(miss));
 #pragma unroll
         for (int i = 0; i < 2 * VPF; ++i) __builtin_amdgcn_sched_group_barrier(SG_DSR, 1, 1);
         static_for<4 * DB>([&](auto ic) __attribute__((always_inline)) {
@@ -309,16 +334,20 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
         });
         __builtin_amdgcn_sched_barrier(0);
         move_reference(mx);
+        idC = idN;
     };
     // the top of a step without the pipeline behind it
     auto meet = [&](int n) __attribute__((always_inline)) {
         top(n, (n + 1) & 1);
+        const int idN = load_ids(n + 4);
         if (n + 1 < nt) {
 #pragma unroll
             for (int i = 0; i < NDMA; ++i) dma_k(dk, i, n & 1);
 #pragma unroll
             for (int i = 0; i < NDMA; ++i) dma_v(dv, i, (n + 1) & 1);
         }
+        advance(n);
+        idC = idN;
     };
 
     using st0 = std::integral_constant<int, 0>;
@@ -326,8 +355,13 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
     f32x16 S0[2], S1[2];
     // prologue: K(0), then K(1) and V(0); scores and reference point of tile 0
     {
-        asm volatile("" : "+v"(idB), "+v"(idC));      // arrived, before the loads that are counted by hand
-        const Desc d0 = descriptors_k(id0, 0), d1 = descriptors_k(idB, 1), e0 = descriptors_v(id0, 0);
+        int i0 = id0, i1 = id1;
+        asm volatile("" : "+v"(i0), "+v"(i1), "+v"(idB), "+v"(idC));      // arrived, before the loads that are counted by hand
+        const Desc d0 = descriptors_k(i0, 0), d1 = descriptors_k(i1, 1), e0 = descriptors_v(i0, 0);
+        const unsigned miss0 = missing(i0, 0);
+        dk = descriptors_k(idB, 2);
+        dv = descriptors_v(i1, 1);
+        miss = missing(i1, 1);
 #pragma unroll
         for (int i = 0; i < NDMA; ++i) dma_k(d0, i, 0);
         if (nt > 1) {
@@ -336,8 +370,10 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
         }
 #pragma unroll
         for (int i = 0; i < NDMA; ++i) dma_v(e0, i, 0);
-        if (nt > 1) wait_vmcnt<2 * NDMA>();           // K(0) has landed; K(1), V(0) may still fly
-        else wait_vmcnt<NDMA>();
+        // the queries, requested before the tiles, are waited for with them: one latency instead of two
+#pragma unroll
+        for (int s = 0; s < DS; ++s) asm volatile("" : "+v"(qf[s]));
+        wait_vmcnt<0>();
         scrub(0);
         __builtin_amdgcn_s_barrier();
         if (tl >= 0) {
@@ -347,7 +383,14 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
                 qk_step(S0, s, 0, 0);
                 qk_step(S0, s, 1, 0);
             }
-            if ((t0 + 1) * BN - 1 > lim0 || miss) mask(S0, t0 * BN, miss);
+#pragma unroll
+            for (int i = 0; i < KPF; ++i) __builtin_amdgcn_sched_group_barrier(SG_DSR, 1, 2);
+            static_for<2 * DS>([&](auto ic) __attribute__((always_inline)) {
+                __builtin_amdgcn_sched_group_barrier(SG_MFMA, 1, 2);
+                if (decltype(ic)::value + KPF < 2 * DS) __builtin_amdgcn_sched_group_barrier(SG_DSR, 1, 2);
+            });
+            __builtin_amdgcn_sched_barrier(0);
+            if ((t0 + 1) * BN - 1 > lim0 || miss0) mask(S0, t0 * BN, miss0);
             move_reference(row_max(S0));
         }
     }
@@ -376,19 +419,24 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
         ++n;
     }
     for (; n < nt; ++n) meet(n);
+    // the ring is free for the next item once every wave is here and nothing flies any more; the output is not waited for
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();
 
     // ---- output.  Accumulator register v of block db is column 32 db + 8 (v / 4) + 4 h + v % 4.
     const float lt = xhalf_sum(l);
     ConstPagedArgs &z = *args_again();
-    if (mine) {
+    const QueryRow x = query_row(z);
+    const int r = x.r, oh = lane_again() >> 5;
+    if (x.mine) {
         if (direct) {
             const float inv = lt > 0.f ? 1.0f / lt : lt == 0.f ? 0.f : lt;      // a row that sees nothing: zeros
-            const int64_t off = hd * z.o_sh + qrow * z.o_sr;
+            const int64_t off = x.head * z.o_sh + x.row * z.o_sr;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int d = 32 * db + 8 * g + 4 * h;
+                    const int d = 32 * db + 8 * g + 4 * oh;
                     if (d >= z.D) continue;
                     f32x4 o;
 #pragma unroll
@@ -402,7 +450,7 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
                         *(f32x4 *)((float *)z.O + off + d) = o;
                     }
                 }
-            if (z.lse && h == 0) z.lse[(int64_t)hd * z.T + qrow] = m * z.scale + logf(lt);
+            if (z.lse && oh == 0) z.lse[(int64_t)x.head * z.T + x.row] = m * z.scale + logf(lt);
         } else {
             float *op = z.Opart + (slot * BM + r) * DK;
 #pragma unroll
@@ -412,17 +460,14 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
                     f32x4 o;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[e] = oacc[db][4 * g + e];
-                    *(f32x4 *)(op + 32 * db + 8 * g + 4 * h) = o;
+                    *(f32x4 *)(op + 32 * db + 8 * g + 4 * oh) = o;
                 }
-            if (h == 0) {
+            if (oh == 0) {
                 z.Mpart[slot * BM + r] = m * z.c;
                 z.Lpart[slot * BM + r] = lt;
             }
         }
     }
-    // the ring is free for the next item once every wave is here and nothing flies any more
-    wait_vmcnt<0>();
-    __builtin_amdgcn_s_barrier();
 }
 
 template <int DU, int NW, bool NT>
@@ -431,7 +476,7 @@ void paged_bf16_kernel(const PagedArgs)
 {
     using C = PagedBf16<DU, NW, NT>;
     __shared__ PlaceLds lds;
-    share_items<NW * 64, C::BN>(xcd_remap(blockIdx.x, gridDim.x), lds, [](const Place &p, int t0, int t1, bool whole, int64_t slot) __attribute__((always_inline)) {
+    share_items<C::BN>(xcd_remap(blockIdx.x, gridDim.x), lds, [](const Place &p, int t0, int t1, bool whole, int64_t slot) __attribute__((always_inline)) {
         paged_bf16_item<DU, NW, NT>(p, t0, t1, whole, slot);
     });
 }

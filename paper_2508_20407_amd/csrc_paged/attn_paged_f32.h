@@ -59,12 +59,12 @@ __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, b
     const int tok0 = p.qb * a.TB;
     const int ntok = min(a.TB, p.q.W - tok0);
     const int r = wave * 32 + j;
-    const int tok = r / a.G, hq = r - tok * a.G;
+    const int tok = (int)(((float)r + 0.5f) * a.per_G), hq = r - tok * a.G;
     const bool mine = tok < ntok;
     const int64_t qrow = p.q.first + tok0 + (mine ? tok : 0);
     const int hd = p.head * a.G + (mine ? hq : 0);
     const int lim = a.causal ? min(len - 1, ctx + tok0 + tok) : len - 1;
-    const int wt0 = wave * 32 / a.G, wt1 = min((wave * 32 + 31) / a.G, ntok - 1);
+    const int wt0 = (int)((wave * 32 + 0.5f) * a.per_G), wt1 = min((int)((wave * 32 + 31.5f) * a.per_G), ntok - 1);
     const int lim0 = uniform(a.causal ? min(len - 1, ctx + tok0 + wt0) : len - 1);
     const int lim1 = uniform(a.causal ? min(len - 1, ctx + tok0 + wt1) : len - 1);
     const int tl = uniform(wt0 >= ntok || lim1 < 0 ? -1 : min(lim1 / BN - t0, nt - 1));
@@ -79,7 +79,7 @@ __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, b
         for (int q = 0; q < DQ; ++q) asm volatile("" : "+v"(qf[q]));
     }
 
-    const int64_t k_rb = a.k_sr * 4, v_rb = a.v_sr * 4;
+    const unsigned k_rb = (unsigned)a.k_sr * 4, v_rb = (unsigned)a.v_sr * 4, kp_b = (unsigned)(a.k_sp * 4), vp_b = (unsigned)(a.v_sp * 4);
     auto kswz = [](int rr) __attribute__((always_inline)) { return rr & 15; };
     auto vswz = [](int rr) __attribute__((always_inline)) { return (rr >> 2 & 1) << 3; };
     unsigned koff[NDMA], voff[NDMA];
@@ -87,8 +87,8 @@ __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, b
     for (int i = 0; i < NDMA; ++i) {
         const int drow = (wave * NDMA + i) * RPI + lane / CPR;
         const int kc = (lane % CPR) ^ kswz(drow), vc = (lane % CPR) ^ vswz(drow);
-        koff[i] = kc >= dchunks ? kNoChunk : (unsigned)((drow & 15) * k_rb) + (kc << 4);
-        voff[i] = vc >= dchunks ? kNoChunk : (unsigned)((drow & 15) * v_rb) + (vc << 4);
+        koff[i] = kc >= dchunks ? kNoChunk : (drow & 15) * k_rb + (kc << 4);
+        voff[i] = vc >= dchunks ? kNoChunk : (drow & 15) * v_rb + (vc << 4);
     }
     const unsigned lds_wave = uniform((int)(lds_offset(Ks) + wave * (NDMA * 1024)));
     const char *const Kg = (const char *)a.K + p.head * a.k_sh * 4;
@@ -103,12 +103,12 @@ __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, b
 #pragma unroll
         for (int g = 0; g < NGW; ++g) {
             const int key = (t0 + n) * BN + 16 * (g0 + g);
-            const int id = __builtin_amdgcn_readlane(ids, g0 + g);
-            const bool there = (unsigned)id < (unsigned)a.P;
-            const int rows = there ? max(min(16, len - key), 0) : 0;
-            const int64_t pr = key & ((1 << a.lr) - 1), pg = there ? id : 0;
-            kd[g] = tile_descriptor(Kg + pg * (a.k_sp * 4) + pr * k_rb, (unsigned)(rows * k_rb));
-            vd[g] = tile_descriptor(Vg + pg * (a.v_sp * 4) + pr * v_rb, (unsigned)(rows * v_rb));
+            const unsigned id = __builtin_amdgcn_readlane(ids, g0 + g);
+            const bool there = id < (unsigned)a.P;
+            const unsigned rows = there ? max(min(16, len - key), 0) : 0, pr = key & ((1 << a.lr) - 1);
+            const uint64_t pg = there ? id : 0;
+            kd[g] = tile_descriptor(Kg + pg * kp_b + pr * k_rb, rows * k_rb);
+            vd[g] = tile_descriptor(Vg + pg * vp_b + pr * v_rb, rows * v_rb);
         }
 #pragma unroll
         for (int i = 0; i < NDMA; ++i) {
@@ -243,7 +243,7 @@ void paged_f32_kernel(const PagedArgs)
 {
     using C = PagedF32<DU, NW>;
     __shared__ PlaceLds lds;
-    share_items<NW * 64, C::BN>(xcd_remap(blockIdx.x, gridDim.x), lds, [](const Place &p, int t0, int t1, bool whole, int64_t slot) __attribute__((always_inline)) {
+    share_items<C::BN>(xcd_remap(blockIdx.x, gridDim.x), lds, [](const Place &p, int t0, int t1, bool whole, int64_t slot) __attribute__((always_inline)) {
         paged_f32_item<DU, NW>(p, t0, t1, whole, slot);
     });
 }

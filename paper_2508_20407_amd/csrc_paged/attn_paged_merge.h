@@ -31,7 +31,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedA
         f32x4 num = {0.f, 0.f, 0.f, 0.f};
         constexpr int NB = 4;
         if (live)
-            for (int k0 = cut.part0 + ln; k0 < cut.part1; k0 += NB * LN) {
+            for (int k0 = ln; k0 < cut.parts; k0 += NB * LN) {
                 float ms[NB], ls[NB];
                 f32x4 os[NB];
 #pragma unroll
@@ -40,7 +40,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedA
                     ls[e] = 0.f;
                     os[e] = f32x4{0.f, 0.f, 0.f, 0.f};
                     const int k = k0 + e * LN;
-                    if (k >= cut.part1) continue;
+                    if (k >= cut.parts) continue;
                     const int64_t slot = 2 * (int64_t)(w + k) + (k == 0);
                     const int64_t idx = slot * BM + r;
                     ms[e] = a.Mpart[idx];

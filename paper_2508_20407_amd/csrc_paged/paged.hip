@@ -82,6 +82,10 @@ tlin_status check_paged(const tlin_paged_params *p)
     const int eb = bytes_of(p->dtype);
     tlin_status st;
     if ((st = check_strides(p->kp_stride, p->D, eb)) || (st = check_strides(p->vp_stride, p->D, eb))) return st;
+    // a page's rows are addressed from its first byte in 32 bits, pages in 64
+    const int64_t most = (int64_t)1 << 32, dense = (int64_t)p->HK * p->page_rows * p->D * eb;
+    if (dense >= most || p->kp_stride[0] * eb >= most || p->vp_stride[0] * eb >= most) return TLIN_ERR_INVALID_ARG;
+    if (p->kp_stride[2] * eb * p->page_rows >= most || p->vp_stride[2] * eb * p->page_rows >= most) return TLIN_ERR_INVALID_ARG;
     return TLIN_OK;
 }
 
@@ -335,8 +339,14 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
     a.M = p->table_width; a.P = p->num_pages; a.lr = log2_of(p->page_rows);
     a.table_stride = p->table_stride ? p->table_stride : p->table_width;
     a.TB = s.tb; a.BM = s.bm();
+    a.by_TB.k = 31;
+    while ((1 << (a.by_TB.k - 31)) < s.tb) ++a.by_TB.k;
+    a.by_TB.m = (uint32_t)((((uint64_t)1 << a.by_TB.k) + s.tb - 1) / s.tb);
     a.shares = s.shares;
-    a.least = 256;
+    a.per_share = 1.0 / s.shares;
+    a.per_G = 1.0f / a.G;
+    a.least = 512;
+    a.start = s.nw == 8 ? 384 : 256;
     a.causal = p->causal != 0;
     a.out_bf16 = p->out_dtype == TLIN_BF16;
     a.scale = p->scale;

@@ -18,6 +18,10 @@
 
 namespace tlin {
 
+// n / d for 0 <= n < 2^31 by a multiplication: m = ceil(2^k / d), k = 31 + ceil(log2 d), from the host.
+struct Divide { uint32_t m; int32_t k; };
+__device__ __forceinline__ int divide(int n, uint32_t m, int k) { return (int)((uint64_t)(uint32_t)n * m >> k); }
+
 struct PagedArgs {
     const void *Q, *K, *V;
     const int32_t *table, *lens, *starts;
@@ -32,8 +36,12 @@ struct PagedArgs {
     int32_t M, P, lr;                    // table width, pages, log2 of a page's rows
     int32_t table_stride;
     int32_t TB, BM;                      // new rows of a query block, rows of a workgroup
+    Divide by_TB;
     int32_t shares;                      // workgroups that the work is cut for
+    double per_share;                    // 1 / shares
+    float per_G;                         // 1 / G: (r + 1/2) / G rounds down to r / G for the rows of a workgroup
     int32_t least;                       // rows of a share at least, a multiple of 64
+    int32_t start;                       // what starting an item costs, in rows of the cache: part of its length in the cuts
     int32_t causal, out_bf16;
     float scale, c;                      // c = scale log2(e)
 };
@@ -41,10 +49,9 @@ struct PagedArgs {
 // The item that a share ends in the middle of: its partials are part 0 in slot 2 w + 1 of that share w, part k in slot
 // 2 (w + k) of the k-th share after it.
 struct CutItem {
-    int32_t rows;            // (new row, query head) pairs; 0: the share ends with its last item, or a share holds all tiles
+    int32_t rows;            // (new row, query head) pairs; 0: the share ends with its last item
     int32_t row, head;       // first new row, first query head
-    int32_t part0, part1;    // the parts that hold tiles: part0 .. part1 - 1
-    int32_t pad[3];
+    int32_t parts;
 };
 
 // The kernel's arguments, to be read again from here on: what is used in one place of a long kernel does not
@@ -57,37 +64,50 @@ __device__ __forceinline__ ConstPagedArgs *args_again()
     return (ConstPagedArgs *)p;
 }
 
-// What starting an item costs (queries, first tiles, output), in rows of the cache: part of its length in the cuts.
-constexpr int kItemRows = 64;
-
 struct Sequence {
     int first, W, len;       // first new row, new rows, rows
     int nqb;                 // query blocks
     int before;              // rows that all of its blocks read (see above)
 };
 
+// a / b for 0 <= a, 0 < b, a / b below 2^20: an approximate quotient is off by at most one
+__device__ __forceinline__ int quotient(int64_t a, int64_t b)
+{
+    int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b));
+    int64_t r = a - q * b;
+    while (r < 0) { --q; r += b; }
+    while (r >= b) { ++q; r -= b; }
+    return q;
+}
+
+template <typename A>
+__device__ __forceinline__ Sequence complete(const A &a, int first, int W, int len)
+{
+    Sequence q;
+    q.first = first;
+    q.W = W;
+    q.len = len;
+    q.nqb = divide(W + a.TB - 1, a.by_TB.m, a.by_TB.k);
+    // (a length below the number of new rows, which no caller means: the rows before the first see nothing)
+    q.before = a.causal ? max(len - W, 0) : max(len, 1);
+    return q;
+}
 template <typename A>
 __device__ __forceinline__ Sequence sequence_of(const A &a, int s)
 {
-    Sequence q;
-    q.first = min(max(a.starts[s], 0), a.T);
-    q.W = max(min(a.starts[s + 1], a.T) - q.first, 0);
-    q.len = (int)min((int64_t)max(a.lens[s], 0), (int64_t)a.M << a.lr);
-    q.nqb = (q.W + a.TB - 1) / a.TB;
-    // (a length below the number of new rows, which no caller means: the rows before the first see nothing)
-    q.before = a.causal ? max(q.len - q.W, 0) : max(q.len, 1);
-    return q;
+    const int first = min(max(a.starts[s], 0), a.T);
+    return complete(a, first, max(min(a.starts[s + 1], a.T) - first, 0), (int)min((int64_t)max(a.lens[s], 0), (int64_t)a.M << a.lr));
 }
 // rows read by block i, and by the first n blocks of a head (n <= nqb), each with its start
 template <typename A>
 __device__ __forceinline__ int64_t block_rows(const A &a, const Sequence &q, int i)
 {
-    return kItemRows + (a.causal ? (int64_t)q.before + min((int64_t)q.W, (int64_t)(i + 1) * a.TB) : (int64_t)q.before);
+    return a.start + (a.causal ? (int64_t)q.before + min((int64_t)q.W, (int64_t)(i + 1) * a.TB) : (int64_t)q.before);
 }
 template <typename A>
 __device__ __forceinline__ int64_t rows_before(const A &a, const Sequence &q, int n)
 {
-    int64_t r = (int64_t)n * (q.before + kItemRows);
+    int64_t r = (int64_t)n * (q.before + a.start);
     if (a.causal) {
         r += (int64_t)a.TB * ((int64_t)n * (n + 1) / 2);
         if (n == q.nqb) r -= (int64_t)n * a.TB - q.W;
@@ -96,7 +116,7 @@ __device__ __forceinline__ int64_t rows_before(const A &a, const Sequence &q, in
 }
 // key tiles of an item up to offset x of its length
 template <int BN>
-__device__ __forceinline__ int tiles_to(int64_t x) { return x <= kItemRows ? 0 : (int)((x - kItemRows + BN - 1) / BN); }
+__device__ __forceinline__ int tiles_to(int64_t x, int start) { return x <= start ? 0 : (int)((x - start + BN - 1) / BN); }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int64_t uniform(int64_t x)
@@ -113,77 +133,101 @@ struct Place {
     Sequence q;
 };
 
-// red, off, s: of the search.  place, left: a wave's own place in its share while it works on an item (kept in scalar
-// registers they were spilled).
-struct PlaceLds { int64_t red[8]; int64_t off; int s; Place place[8]; int64_t left[8]; };
+// place, left: a wave's own place in its share while it works on an item (kept in scalar registers they were spilled).
+// first, W, len: the sequences, where there are at most 64 of them.
+struct PlaceLds { Place place[8]; int64_t left[8]; int first[64], W[64], len[64]; };
 
-// The item at position w * quota, for a workgroup of NT threads (false: w is behind the last share).
-template <int NT, typename A>
+// Sum over this lane and those below it, by lane moves inside the vector unit.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t moved(int64_t x)
+{
+    const int lo = __builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+    const int hi = __builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROWS, 0xf, false);
+    return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
+}
+__device__ __forceinline__ int64_t wave_scan(int64_t x)
+{
+    x += moved<0x111, 0xf>(x);      // row_shr 1, 2, 4, 8: inside sixteen lanes
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    x += moved<0x118, 0xf>(x);
+    x += moved<0x142, 0xa>(x);      // the last lane of a row of sixteen to the next row (rows 1 and 3)
+    x += moved<0x143, 0xc>(x);      // lane 31 to rows 2 and 3
+    return x;
+}
+__device__ __forceinline__ int64_t from_lane(int64_t x, int lane)
+{
+    const unsigned lo = __builtin_amdgcn_readlane((int)x, lane), hi = __builtin_amdgcn_readlane((int)(x >> 32), lane);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// The item at position w * quota (false: w is behind the last share).  Every wave computes it for itself, a lane a run of
+// sequences: no barrier, and one latency of memory where there are at most 64.
+template <typename A>
 __device__ __forceinline__ bool find_place(const A &a, int w, Place &p, PlaceLds &lds)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int run = (a.S + NT - 1) / NT;       // sequences of a thread, next to each other
-    const int lo = min(tid * run, a.S), hi = min(lo + run, a.S);
+    const int lane = threadIdx.x & 63;
+    const int run = (a.S + 63) >> 6;
+    const int lo = min(lane * run, a.S), hi = min(lo + run, a.S);
     int64_t sum = 0;
-    for (int s = lo; s < hi; ++s) {
-        const Sequence q = sequence_of(a, s);
-        sum += a.HK * rows_before(a, q, q.nqb);
+    Sequence q = {};
+    if (run == 1) {
+        if (lo < hi) {
+            q = sequence_of(a, lo);
+            sum = a.HK * rows_before(a, q, q.nqb);
+        }
+        // (every wave writes the same)
+        lds.first[lane] = q.first; lds.W[lane] = q.W; lds.len[lane] = q.len;
+    } else {
+#pragma unroll 4
+        for (int s = lo; s < hi; ++s) {
+            const Sequence o = sequence_of(a, s);
+            sum += a.HK * rows_before(a, o, o.nqb);
+        }
     }
-    int64_t upto = sum;
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-        const int64_t y = __shfl_up(upto, off);
-        if (lane >= off) upto += y;
-    }
-    if (lane == 63) lds.red[wave] = upto;
-    __syncthreads();
-    int64_t total = 0, before = upto - sum;
-#pragma unroll
-    for (int k = 0; k < NT / 64; ++k) {
-        before += k < wave ? lds.red[k] : 0;
-        total += lds.red[k];
-    }
-    p.total = uniform(total);
-    const int64_t even = (p.total + a.shares - 1) / a.shares;
+    const int64_t upto = wave_scan(sum);
+    p.total = from_lane(upto, 63);
+    // any length that no more than `shares` shares of it are needed for
+    const int64_t even = (int64_t)((double)p.total * a.per_share) + 1;
     p.quota = uniform(even <= a.least ? (int64_t)a.least : (even + 63) / 64 * 64);
     const int64_t pos = w * p.quota;
     if (pos >= p.total) return false;
-    if (pos >= before && pos < before + sum) {
-        int64_t at = before;
-        for (int s = lo; s < hi; ++s) {
-            const Sequence q = sequence_of(a, s);
-            const int64_t n = a.HK * rows_before(a, q, q.nqb);
-            if (pos < at + n) {
-                lds.s = s;
-                lds.off = pos - at;
-                break;
-            }
-            at += n;
+    const uint64_t holds = __builtin_amdgcn_ballot_w64(pos < upto && pos >= upto - sum);
+    const int owner = __builtin_ctzll(holds);
+    int64_t off = pos - from_lane(upto - sum, owner);
+    int s = owner;
+    if (run > 1) {
+        s = owner * run;
+        for (;; ++s) {
+            q = sequence_of(a, s);
+            const int64_t n = uniform(a.HK * rows_before(a, q, q.nqb));
+            if (off < n) break;
+            off -= n;
         }
+        p.q.first = uniform(q.first); p.q.W = uniform(q.W); p.q.len = uniform(q.len); p.q.nqb = uniform(q.nqb); p.q.before = uniform(q.before);
+    } else {
+        p.q.first = __builtin_amdgcn_readlane(q.first, owner); p.q.W = __builtin_amdgcn_readlane(q.W, owner);
+        p.q.len = __builtin_amdgcn_readlane(q.len, owner); p.q.nqb = __builtin_amdgcn_readlane(q.nqb, owner);
+        p.q.before = __builtin_amdgcn_readlane(q.before, owner);
     }
-    __syncthreads();
-    p.s = uniform(lds.s);
-    int64_t off = uniform(lds.off);
-    Sequence q = sequence_of(a, p.s);
-    q.first = uniform(q.first); q.W = uniform(q.W); q.len = uniform(q.len); q.nqb = uniform(q.nqb); q.before = uniform(q.before);
-    p.q = q;
-    const int64_t head = rows_before(a, q, q.nqb);
-    p.head = uniform((int)(off / head));
+    p.s = s;
+    const int64_t head = rows_before(a, p.q, p.q.nqb);
+    p.head = uniform(quotient(off, head));
     off -= p.head * head;
-    int lo_b = 0, hi_b = q.nqb - 1;            // the last block that begins at or before off
+    int lo_b = 0, hi_b = p.q.nqb - 1;          // the last block that begins at or before off
     while (lo_b < hi_b) {
         const int mid = (lo_b + hi_b + 1) >> 1;
-        if (rows_before(a, q, mid) <= off) lo_b = mid;
+        if (rows_before(a, p.q, mid) <= off) lo_b = mid;
         else hi_b = mid - 1;
     }
     p.qb = uniform(lo_b);
-    p.x = uniform(off - rows_before(a, q, p.qb));
+    p.x = uniform(off - rows_before(a, p.q, p.qb));
     return true;
 }
 
 // The item after (s, head, qb); the caller knows that there is one.
 template <typename A>
-__device__ __forceinline__ void next_item(const A &a, Place &p)
+__device__ __forceinline__ void next_item(const A &a, Place &p, const PlaceLds &lds)
 {
     p.x = 0;
     if (++p.qb < p.q.nqb) return;
@@ -192,64 +236,72 @@ __device__ __forceinline__ void next_item(const A &a, Place &p)
     p.head = 0;
     do {
         ++p.s;
-        const Sequence q = sequence_of(a, p.s);
+        const Sequence q = a.S <= 64 ? complete(a, lds.first[p.s], lds.W[p.s], lds.len[p.s]) : sequence_of(a, p.s);
         p.q.first = uniform(q.first); p.q.W = uniform(q.W); p.q.len = uniform(q.len); p.q.nqb = uniform(q.nqb); p.q.before = uniform(q.before);
     } while (p.q.nqb == 0 && p.s + 1 < a.S);
 }
 
+// Rows that a cut leaves of an item behind it at least.
+constexpr int kShortest = 128;
+
 // The items of share w, one after another: work(place, first tile, last tile, whole, slot) for each, and the record of
-// the one that the share ends in the middle of.
-template <int NT, int BN, typename F>
+// the one that the share ends in the middle of.  A cut that would leave no whole tile of an item before it is moved to the
+// item's beginning, one that would leave less than kShortest rows behind it to its end, by both of its neighbours alike:
+// such a piece would cost more to start than to do, and every piece that is left holds a tile.
+template <int BN, typename F>
 __device__ __forceinline__ void share_items(int w, PlaceLds &lds, F work)
 {
     const int wave = uniform((int)threadIdx.x >> 6);
     ConstPagedArgs &a = *args_again();
     Place p;
     CutItem cut = {};
-    const bool any = find_place<NT>(a, w, p, lds);
-    if (any) {
-        int64_t left = min(p.quota, p.total - w * p.quota);
-        for (;;) {
-            int64_t n;
-            {
-                ConstPagedArgs &b = *args_again();
-                n = block_rows(b, p.q, p.qb);
+    if (find_place(a, w, p, lds)) {
+        int64_t left = min(p.quota, p.total - w * p.quota);      // to the end of the share, as it was cut
+        bool more = true;
+        {
+            const int64_t n = block_rows(a, p.q, p.qb);
+            if (p.x < a.start + BN) {
+                left += p.x;
+                p.x = 0;
+            } else if (n - p.x < kShortest) {
+                left -= n - p.x;
+                more = left > 0;
+                if (more) next_item(a, p, lds);
             }
-            const int64_t x1 = min(n, p.x + left);
-            const int t0 = tiles_to<BN>(p.x), t1 = tiles_to<BN>(x1), nt = tiles_to<BN>(n);
-            if (t0 < t1) {
-                lds.place[wave] = p;
-                lds.left[wave] = left;
-                work(p, t0, t1, t0 == 0 && t1 == nt, 2 * w + (p.x > 0 ? 0 : 1));
-                asm volatile("" ::: "memory");
-                const Place &o = lds.place[wave];
-                p.total = uniform(o.total); p.quota = uniform(o.quota);
-                p.s = uniform(o.s); p.head = uniform(o.head); p.qb = uniform(o.qb); p.x = uniform(o.x);
-                p.q.first = uniform(o.q.first); p.q.W = uniform(o.q.W); p.q.len = uniform(o.q.len);
-                p.q.nqb = uniform(o.q.nqb); p.q.before = uniform(o.q.before);
-                left = uniform(lds.left[wave]);
-            }
+        }
+        while (more) {
             ConstPagedArgs &b = *args_again();
-            const int64_t len = block_rows(b, p.q, p.qb), x = min(len, p.x + left);
-            left -= x - p.x;
-            if (left <= 0) {
-                // the cut goes through an item that begins here
-                if (x < len && p.x == 0) {
-                    const int tiles = tiles_to<BN>(len), tile1 = tiles_to<BN>(x);
-                    const int last = (int)((len - x + p.quota - 1) / p.quota);       // shares after this one with a part of it
-                    // (a part is empty where it ends before the first tile, or begins behind the last)
-                    const int part0 = tile1 == 0, part1 = tiles_to<BN>(x + (last - 1) * p.quota) < tiles ? last + 1 : last;
-                    if (part1 - part0 > 1) {
-                        cut.rows = min(b.TB, p.q.W - p.qb * b.TB) * b.G;
-                        cut.row = p.q.first + p.qb * b.TB;
-                        cut.head = p.head * b.G;
-                        cut.part0 = part0;
-                        cut.part1 = part1;
-                    }
-                }
-                break;
+            const int start = b.start;
+            const int64_t n = block_rows(b, p.q, p.qb), to = p.x + left;
+            if (to < n && to < start + BN) break;                // (so p.x is 0) the next share's, from its beginning
+            const bool all = n - to < kShortest;                 // up to its end
+            const int64_t x1 = all ? n : to;
+            const int t0 = tiles_to<BN>(p.x, start), t1 = tiles_to<BN>(x1, start);
+            lds.place[wave] = p;
+            lds.left[wave] = left;
+            work(p, t0, t1, p.x == 0 && all, 2 * w + (p.x == 0));
+            asm volatile("" ::: "memory");
+            const Place &o = lds.place[wave];
+            p.total = uniform(o.total); p.quota = uniform(o.quota);
+            p.s = uniform(o.s); p.head = uniform(o.head); p.qb = uniform(o.qb); p.x = uniform(o.x);
+            p.q.first = uniform(o.q.first); p.q.W = uniform(o.q.W); p.q.len = uniform(o.q.len);
+            p.q.nqb = uniform(o.q.nqb); p.q.before = uniform(o.q.before);
+            left = uniform(lds.left[wave]);
+            ConstPagedArgs &c = *args_again();
+            const int64_t len = block_rows(c, p.q, p.qb), end = p.x + left;
+            if (end >= len) {
+                left = end - len;
+                if (left == 0) break;
+                next_item(c, p, lds);
+                continue;
             }
-            next_item(b, p);
+            if (p.x == 0 && len - end >= kShortest) {            // the cut goes through an item that begins here
+                cut.rows = min(c.TB, p.q.W - p.qb * c.TB) * c.G;
+                cut.row = p.q.first + p.qb * c.TB;
+                cut.head = p.head * c.G;
+                cut.parts = quotient(len - kShortest - end, p.quota) + 2;
+            }
+            break;
         }
     }
     if (threadIdx.x == 0) args_again()->cuts[w] = cut;
