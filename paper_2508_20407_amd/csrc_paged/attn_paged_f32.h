@@ -133,6 +133,7 @@ __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, b
 #pragma unroll
         for (int v = 0; v < 16; ++v) oacc[db][v] = 0.f;
     const float thr = 8.0f / a.c;
+    const int D = a.D;
 
     asm volatile("" : "+v"(idA), "+v"(idB));
     unsigned miss = missing(idA, 0);
@@ -155,6 +156,7 @@ __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, b
         for (int v = 0; v < 16; ++v) S[v] = 0.f;
 #pragma unroll
         for (int q = 0; q < DQ; ++q) {
+            if (q >= DQ - 3 && 8 * q >= D) continue;      // (uniform; columns are computed in blocks of 32, contracted in steps of 8)
             const f32x4 kf = *(lds_f32x4 *)(uintptr_t)(kaddr[q] + st);
 #pragma unroll
             for (int e = 0; e < 4; ++e) S = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[q][e], S, 0, 0, 0);
@@ -238,7 +240,7 @@ __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, b
 }
 
 template <int DU, int NW>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 8)))
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 8)))
 void paged_f32_kernel(const PagedArgs)
 {
     using C = PagedF32<DU, NW>;

@@ -3,7 +3,7 @@
 // A cache's book is small (a table entry a page and sequence, a count a page) and these kernels are bound by the latency of
 // dependent steps, so each does its work in as few launches as its dependences allow: free and fork a workgroup a
 // sequence (counts by integer atomics, whose order changes nothing), reserve one workgroup that scans, compact three
-// launches over the pages.  Copies are bound by HBM.
+// launches over the pages (two where there are few).  Copies are bound by HBM.
 #pragma once
 #include "common.h"
 
@@ -20,7 +20,7 @@ struct BookArgs {
     int32_t stride;              // of the table
     // compact
     const int32_t *table_in, *refs_in;
-    int32_t nblocks;
+    int32_t nblocks, counted;    // blocks of pages, and whether pages_count_kernel has counted them
 };
 
 __device__ __forceinline__ bool names_page(int id, int P) { return id >= 0 && id < P; }
@@ -133,9 +133,11 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(const BookArgs a)
 
     // pages wanted before every sequence: 32-bit sums would do for the pages there are, not for those asked for
     int64_t asked = 0;
+    Need mine = {0, 0, 0, false};        // where each thread has one sequence at most
     for (int s0 = 0; s0 < a.S; s0 += 1024) {
         const int s = s0 + tid;
         const Need n = s < a.S ? need_of(a, s) : Need{0, 0, 0, false};
+        mine = n;
         int64_t all;
         const int64_t at = asked + block_scan<int64_t>(n.bad ? 0 : n.pages, all, red);
         if (s < a.S) first[s] = (int)min(at, (int64_t)a.P + 1);
@@ -168,7 +170,7 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(const BookArgs a)
     int copies = 0;
     for (int s0 = 0; s0 < a.S; s0 += 1024) {
         const int s = s0 + tid;
-        const Need n = s < a.S ? need_of(a, s) : Need{0, 0, 0, false};
+        const Need n = a.S <= 1024 ? mine : s < a.S ? need_of(a, s) : Need{0, 0, 0, false};
         const bool ok = s < a.S && !n.bad && (n.pages == 0 || (int64_t)first[s] + n.pages <= avail);
         int all;
         const int at = copies + block_scan<int>(ok ? n.copy : 0, all, red32);
@@ -231,10 +233,19 @@ __global__ __launch_bounds__(1024) void pages_plan_kernel(const BookArgs a)
     __shared__ int red[16];
     const int tid = threadIdx.x, b = blockIdx.x;
     int before = 0, live = 0, all;
-    for (int k = tid; k < a.nblocks; k += 1024) {
-        const int c = a.scratch[k];
-        before += k < b ? c : 0;
-        live += c;
+    if (a.counted) {
+        for (int k = tid; k < a.nblocks; k += 1024) {
+            const int c = a.scratch[k];
+            before += k < b ? c : 0;
+            live += c;
+        }
+    } else {
+#pragma unroll 8
+        for (int k = tid; k < a.P; k += 1024) {
+            const int c = a.refs_in[k] > 0;
+            before += k < b * kPagesPerBlock ? c : 0;
+            live += c;
+        }
     }
     block_scan<int>(before, all, red);
     const int base = all;
@@ -348,10 +359,10 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(const CopyArgs a)
             u32x4 x[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (i + u * 256 < hi) x[u] = *(const u32x4 *)(src + at(i + u * 256));
+                if (i + u * 256 < hi) x[u] = __builtin_nontemporal_load((const u32x4 *)(src + at(i + u * 256)));
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (i + u * 256 < hi) *(u32x4 *)(dst + at(i + u * 256)) = x[u];
+                if (i + u * 256 < hi) __builtin_nontemporal_store(x[u], (u32x4 *)(dst + at(i + u * 256)));
         }
     }
 }

@@ -144,8 +144,8 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a)
             store_piece<T, E>(y + u * E, p, a.D - u * E);
         } else if (u < turned) {
             Pack<T, E> p1, p2;
-            p1.raw = *(const typename Piece<E * sizeof(T)>::type *)(x + u * E);
-            p2.raw = *(const typename Piece<E * sizeof(T)>::type *)(x + half + u * E);
+            p1.raw = __builtin_nontemporal_load((const typename Piece<E * sizeof(T)>::type *)(x + u * E));
+            p2.raw = __builtin_nontemporal_load((const typename Piece<E * sizeof(T)>::type *)(x + half + u * E));
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const float2 w = cs[t][u * E + e];
@@ -153,8 +153,8 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a)
                 p1.e[e] = (T)(x1 * w.x - x2 * w.y);
                 p2.e[e] = (T)(x1 * w.y + x2 * w.x);
             }
-            *(typename Piece<E * sizeof(T)>::type *)(y + u * E) = p1.raw;
-            *(typename Piece<E * sizeof(T)>::type *)(y + half + u * E) = p2.raw;
+            __builtin_nontemporal_store(p1.raw, (typename Piece<E * sizeof(T)>::type *)(y + u * E));
+            __builtin_nontemporal_store(p2.raw, (typename Piece<E * sizeof(T)>::type *)(y + half + u * E));
         } else {
             const int col = a.rot + (u - turned) * E;
             Pack<T, E> p;
