@@ -2,6 +2,7 @@
 #include "host.h"
 #include "attn_paged_bf16.h"
 #include "attn_paged_f32.h"
+#include "attn_paged_f32_few.h"
 #include "attn_paged_merge.h"
 #include "pages.h"
 #include "rope.h"
@@ -109,7 +110,7 @@ BookArgs book_args(const tlin_book_params *p)
 // ---- attention
 
 // Waves of a workgroup (32 rows each) and what follows from them.
-struct PagedShape { int nw, shares, dk, tb; int bm() const { return nw * 32; } };
+struct PagedShape { int nw, shares, dk, tb; bool few; int bm() const { return few ? kFewRows : nw * 32; } };
 
 int group_of(const tlin_paged_params *p) { return p->H / p->HK; }
 
@@ -125,6 +126,12 @@ PagedShape paged_shape(const tlin_paged_params *p)
     s.dk = p->D <= 64 ? 64 : 128;
     s.nw = rows <= 64 ? 2 : rows <= 128 || s.dk == 64 || !bf ? 4 : 8;
     s.shares = s.nw == 8 ? kNumCU : s.dk == 128 ? 2 * kNumCU : 3 * kNumCU;
+    // up to sixteen fp32 rows: waves on their own, two to a SIMD
+    s.few = !bf && rows <= kFewRows;
+    if (s.few) {
+        s.nw = 4;
+        s.shares = 8 * kNumCU;
+    }
     s.tb = s.bm() / group_of(p);
     return s;
 }
@@ -157,6 +164,11 @@ tlin_status launch_paged_f32(const PagedArgs &a, hipStream_t st)
     static std::atomic<uint64_t> allowed{0};
     tlin_status s = allow_lds(kernel, lds, allowed);
     return s ? s : launch_kernel(kernel, dim3(a.shares), dim3(NW * 64), lds, st, a);
+}
+template <int DK>
+tlin_status launch_paged_few(const PagedArgs &a, hipStream_t st)
+{
+    return launch_kernel((const void *)paged_f32_few_kernel<DK>, dim3(a.shares / 4), dim3(256), 0, st, a);
 }
 template <int DU>
 tlin_status launch_paged(const PagedArgs &a, const PagedShape &s, bool bf, bool nt, hipStream_t st)
@@ -358,7 +370,8 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
     const int64_t named = (int64_t)p->S * p->table_width, most = named < p->num_pages ? named : p->num_pages;
     const bool nt = p->max_rows <= s.tb && most * p->HK * p->page_rows * p->D * 4 >= (int64_t)192 << 20;
     const int du = (p->D + 31) / 32 * 32;
-    st = du == 32 ? launch_paged<32>(a, s, bf, nt, hs) : du == 64 ? launch_paged<64>(a, s, bf, nt, hs)
+    st = s.few ? (s.dk == 64 ? launch_paged_few<64>(a, hs) : launch_paged_few<128>(a, hs))
+         : du == 32 ? launch_paged<32>(a, s, bf, nt, hs) : du == 64 ? launch_paged<64>(a, s, bf, nt, hs)
          : du == 96 ? launch_paged<96>(a, s, bf, nt, hs) : launch_paged<128>(a, s, bf, nt, hs);
     if (st) return st;
     const int64_t items = (int64_t)p->S * p->HK * ((p->max_rows + s.tb - 1) / s.tb);

@@ -304,7 +304,7 @@ __device__ __forceinline__ void share_items(int w, PlaceLds &lds, F work)
             break;
         }
     }
-    if (threadIdx.x == 0) args_again()->cuts[w] = cut;
+    if ((threadIdx.x & 63) == 0) args_again()->cuts[w] = cut;      // (every wave that has this share writes the same)
 }
 
 }  // namespace tlin
