@@ -40,8 +40,7 @@ struct PagedArgs {
     int32_t shares;                      // workgroups that the work is cut for
     double per_share;                    // 1 / shares
     float per_G;                         // 1 / G: (r + 1/2) / G rounds down to r / G for the rows of a workgroup
-    int32_t least;                       // rows of a share at least, a multiple of 64
-    int32_t start;                       // what starting an item costs, in rows of the cache: part of its length in the cuts
+    int32_t start;                       // what starting an item costs, in rows of the cache (even)
     int32_t causal, out_bf16;
     float scale, c;                      // c = scale log2(e)
 };
@@ -63,6 +62,9 @@ __device__ __forceinline__ ConstPagedArgs *args_again()
     asm volatile("" : "+s"(p));
     return (ConstPagedArgs *)p;
 }
+
+// Rows that a cut leaves of an item behind it at least.
+constexpr int kShortest = 128;
 
 struct Sequence {
     int first, W, len;       // first new row, new rows, rows
@@ -98,16 +100,16 @@ __device__ __forceinline__ Sequence sequence_of(const A &a, int s)
     const int first = min(max(a.starts[s], 0), a.T);
     return complete(a, first, max(min(a.starts[s + 1], a.T) - first, 0), (int)min((int64_t)max(a.lens[s], 0), (int64_t)a.M << a.lr));
 }
-// rows read by block i, and by the first n blocks of a head (n <= nqb), each with its start
+// rows read by block i, and by the first n blocks of a head (n <= nqb)
 template <typename A>
 __device__ __forceinline__ int64_t block_rows(const A &a, const Sequence &q, int i)
 {
-    return a.start + (a.causal ? (int64_t)q.before + min((int64_t)q.W, (int64_t)(i + 1) * a.TB) : (int64_t)q.before);
+    return a.causal ? (int64_t)q.before + min((int64_t)q.W, (int64_t)(i + 1) * a.TB) : (int64_t)q.before;
 }
 template <typename A>
 __device__ __forceinline__ int64_t rows_before(const A &a, const Sequence &q, int n)
 {
-    int64_t r = (int64_t)n * (q.before + a.start);
+    int64_t r = (int64_t)n * q.before;
     if (a.causal) {
         r += (int64_t)a.TB * ((int64_t)n * (n + 1) / 2);
         if (n == q.nqb) r -= (int64_t)n * a.TB - q.W;
@@ -127,7 +129,8 @@ __device__ __forceinline__ int64_t uniform(int64_t x)
 
 // Where a share begins, and how the shares are cut.
 struct Place {
-    int64_t total, quota;    // rows in all, rows of a share
+    int64_t total, quota;    // length of all items, of a share
+    int start;               // what starting an item counts for in its length
     int s, head, qb;         // the item at the position asked for
     int64_t x;               // offset of the position inside that item
     Sequence q;
@@ -169,12 +172,13 @@ __device__ __forceinline__ bool find_place(const A &a, int w, Place &p, PlaceLds
     const int lane = threadIdx.x & 63;
     const int run = (a.S + 63) >> 6;
     const int lo = min(lane * run, a.S), hi = min(lo + run, a.S);
-    int64_t sum = 0;
+    int64_t rows = 0, items = 0;
     Sequence q = {};
     if (run == 1) {
         if (lo < hi) {
             q = sequence_of(a, lo);
-            sum = a.HK * rows_before(a, q, q.nqb);
+            rows = a.HK * rows_before(a, q, q.nqb);
+            items = (int64_t)a.HK * q.nqb;
         }
         // (every wave writes the same)
         lds.first[lane] = q.first; lds.W[lane] = q.W; lds.len[lane] = q.len;
@@ -182,14 +186,21 @@ __device__ __forceinline__ bool find_place(const A &a, int w, Place &p, PlaceLds
 #pragma unroll 4
         for (int s = lo; s < hi; ++s) {
             const Sequence o = sequence_of(a, s);
-            sum += a.HK * rows_before(a, o, o.nqb);
+            rows += a.HK * rows_before(a, o, o.nqb);
+            items += (int64_t)a.HK * o.nqb;
         }
     }
-    const int64_t upto = wave_scan(sum);
+    const int64_t rows_to = wave_scan(rows), items_to = wave_scan(items);
+    // Where the chip has more workgroups than there is work for, a start costs less, as no other workgroup waits for the
+    // memory it waits for, and shares may be shorter: half of its price (16 sequences of up to 900 rows, 8 key heads x 128: 27
+    // -> 22 us; 64 sequences of up to 1000 rows, with it: 41 -> 47).
+    const int64_t all = from_lane(rows_to, 63);
+    p.start = all < (int64_t)a.shares * a.start ? a.start / 2 : a.start;
+    const int64_t sum = rows + items * p.start, upto = rows_to + items_to * p.start;
     p.total = from_lane(upto, 63);
     // any length that no more than `shares` shares of it are needed for
     const int64_t even = (int64_t)((double)p.total * a.per_share) + 1;
-    p.quota = uniform(even <= a.least ? (int64_t)a.least : (even + 63) / 64 * 64);
+    p.quota = uniform(max((even + 63) / 64 * 64, (int64_t)p.start + kShortest));
     const int64_t pos = w * p.quota;
     if (pos >= p.total) return false;
     const uint64_t holds = __builtin_amdgcn_ballot_w64(pos < upto && pos >= upto - sum);
@@ -200,7 +211,7 @@ __device__ __forceinline__ bool find_place(const A &a, int w, Place &p, PlaceLds
         s = owner * run;
         for (;; ++s) {
             q = sequence_of(a, s);
-            const int64_t n = uniform(a.HK * rows_before(a, q, q.nqb));
+            const int64_t n = uniform(a.HK * (rows_before(a, q, q.nqb) + (int64_t)q.nqb * p.start));
             if (off < n) break;
             off -= n;
         }
@@ -211,17 +222,17 @@ __device__ __forceinline__ bool find_place(const A &a, int w, Place &p, PlaceLds
         p.q.before = __builtin_amdgcn_readlane(q.before, owner);
     }
     p.s = s;
-    const int64_t head = rows_before(a, p.q, p.q.nqb);
+    const int64_t head = rows_before(a, p.q, p.q.nqb) + (int64_t)p.q.nqb * p.start;
     p.head = uniform(quotient(off, head));
     off -= p.head * head;
     int lo_b = 0, hi_b = p.q.nqb - 1;          // the last block that begins at or before off
     while (lo_b < hi_b) {
         const int mid = (lo_b + hi_b + 1) >> 1;
-        if (rows_before(a, p.q, mid) <= off) lo_b = mid;
+        if (rows_before(a, p.q, mid) + (int64_t)mid * p.start <= off) lo_b = mid;
         else hi_b = mid - 1;
     }
     p.qb = uniform(lo_b);
-    p.x = uniform(off - rows_before(a, p.q, p.qb));
+    p.x = uniform(off - rows_before(a, p.q, p.qb) - (int64_t)p.qb * p.start);
     return true;
 }
 
@@ -241,9 +252,6 @@ __device__ __forceinline__ void next_item(const A &a, Place &p, const PlaceLds &
     } while (p.q.nqb == 0 && p.s + 1 < a.S);
 }
 
-// Rows that a cut leaves of an item behind it at least.
-constexpr int kShortest = 128;
-
 // The items of share w, one after another: work(place, first tile, last tile, whole, slot) for each, and the record of
 // the one that the share ends in the middle of.  A cut that would leave no whole tile of an item before it is moved to the
 // item's beginning, one that would leave less than kShortest rows behind it to its end, by both of its neighbours alike:
@@ -259,8 +267,8 @@ __device__ __forceinline__ void share_items(int w, PlaceLds &lds, F work)
         int64_t left = min(p.quota, p.total - w * p.quota);      // to the end of the share, as it was cut
         bool more = true;
         {
-            const int64_t n = block_rows(a, p.q, p.qb);
-            if (p.x < a.start + BN) {
+            const int64_t n = block_rows(a, p.q, p.qb) + p.start;
+            if (p.x < p.start + BN) {
                 left += p.x;
                 p.x = 0;
             } else if (n - p.x < kShortest) {
@@ -271,8 +279,8 @@ __device__ __forceinline__ void share_items(int w, PlaceLds &lds, F work)
         }
         while (more) {
             ConstPagedArgs &b = *args_again();
-            const int start = b.start;
-            const int64_t n = block_rows(b, p.q, p.qb), to = p.x + left;
+            const int start = p.start;
+            const int64_t n = block_rows(b, p.q, p.qb) + start, to = p.x + left;
             if (to < n && to < start + BN) break;                // (so p.x is 0) the next share's, from its beginning
             const bool all = n - to < kShortest;                 // up to its end
             const int64_t x1 = all ? n : to;
@@ -282,13 +290,13 @@ __device__ __forceinline__ void share_items(int w, PlaceLds &lds, F work)
             work(p, t0, t1, p.x == 0 && all, 2 * w + (p.x == 0));
             asm volatile("" ::: "memory");
             const Place &o = lds.place[wave];
-            p.total = uniform(o.total); p.quota = uniform(o.quota);
+            p.total = uniform(o.total); p.quota = uniform(o.quota); p.start = uniform(o.start);
             p.s = uniform(o.s); p.head = uniform(o.head); p.qb = uniform(o.qb); p.x = uniform(o.x);
             p.q.first = uniform(o.q.first); p.q.W = uniform(o.q.W); p.q.len = uniform(o.q.len);
             p.q.nqb = uniform(o.q.nqb); p.q.before = uniform(o.q.before);
             left = uniform(lds.left[wave]);
             ConstPagedArgs &c = *args_again();
-            const int64_t len = block_rows(c, p.q, p.qb), end = p.x + left;
+            const int64_t len = block_rows(c, p.q, p.qb) + p.start, end = p.x + left;
             if (end >= len) {
                 left = end - len;
                 if (left == 0) break;
