@@ -444,8 +444,11 @@ tlin_status tlin_pages_compact(const tlin_book_params *p, const int32_t *table, 
     // Up to 32768 pages every block of the plan counts all of them itself (32 loads a thread that travel together, about
     // 1 us) instead of waiting for a launch of counts (5 us).
     a.counted = p->num_pages > 32768;
+    // A book of one block of pages and few table entries is done by the plan's workgroup.
+    a.alone = a.nblocks == 1 && (int64_t)p->S * p->table_width <= 16384;
     if (a.counted && (st = launch_kernel((const void *)pages_count_kernel, dim3(a.nblocks), dim3(1024), 0, hs, a))) return st;
     if ((st = launch_kernel((const void *)pages_plan_kernel, dim3(a.nblocks), dim3(1024), 0, hs, a))) return st;
+    if (a.alone) return TLIN_OK;
     const int64_t entries = (int64_t)p->S * p->table_width > p->num_pages ? (int64_t)p->S * p->table_width : p->num_pages;
     const int64_t blocks = (entries + 255) / 256;
     return launch_kernel((const void *)pages_apply_kernel, dim3((unsigned)(blocks < 8 * kNumCU ? blocks : 8 * kNumCU)), dim3(256), 0, hs, a);

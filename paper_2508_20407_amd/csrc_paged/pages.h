@@ -21,6 +21,7 @@ struct BookArgs {
     // compact
     const int32_t *table_in, *refs_in;
     int32_t nblocks, counted;    // blocks of pages, and whether pages_count_kernel has counted them
+    int32_t alone;               // the plan's one workgroup applies it too
 };
 
 __device__ __forceinline__ bool names_page(int id, int P) { return id >= 0 && id < P; }
@@ -225,6 +226,39 @@ __global__ __launch_bounds__(1024) void pages_count_kernel(const BookArgs a)
     if (threadIdx.x == 0) a.scratch[blockIdx.x] = all;
 }
 
+// The table and the counts after the moves, and the entries of moves behind the last: entries i0, i0 + step, ...  Tables and
+// counts may be written in place: an entry is read and written by one thread, a hole's count and that of the page that
+// moves into it by the hole's.
+__device__ __forceinline__ void apply_moves(const BookArgs &a, int64_t i0, int64_t step)
+{
+    const int32_t *rank = a.scratch + a.nblocks;
+    const int L = a.scratch[a.nblocks + a.P], K = a.count[0];
+    for (int64_t i = i0; i < (int64_t)a.S * a.M; i += step) {
+        const int64_t s = i / a.M, at = s * a.stride + (i - s * a.M);
+        int id = a.table_in[at];
+        // (a page that a table names and whose count is 0 goes nowhere: the entry stays)
+        if (id >= L && id < a.P && rank[id] >= 0) id = a.moves[2 * rank[id] + 1];
+        a.table[at] = id;
+    }
+    for (int64_t i = i0; i < a.P; i += step) {
+        const int id = (int)i, n = a.refs_in[id];
+        if (id < L) {
+            if (n > 0) a.refs[id] = n;
+            else {
+                const int from = a.moves[2 * rank[id]];
+                const int m = a.refs_in[from];
+                a.refs[id] = m;
+                a.refs[from] = 0;
+            }
+        } else if (n <= 0) a.refs[id] = 0;
+        if (id >= K && id < a.P / 2) a.moves[2 * id] = a.moves[2 * id + 1] = -1;
+    }
+}
+__global__ __launch_bounds__(256) void pages_apply_kernel(const BookArgs a)
+{
+    apply_moves(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+}
+
 // With L live pages in all, the hole below L of rank i (holes counted from the lowest) takes the live page whose
 // rank among the live ones is L - 1 - i.  rank[page] (behind the block counts) keeps i for holes
 // below L and pages that move, -1 for free pages from L on.
@@ -282,35 +316,9 @@ __global__ __launch_bounds__(1024) void pages_plan_kernel(const BookArgs a)
     }
     if (L == 0 && b == 0 && tid == 0) a.count[0] = 0;
     if (b == 0 && tid == 0) a.scratch[a.nblocks + a.P] = L;
-}
-
-// The table and the counts after the moves, and the entries of moves behind the last.  Tables and counts may be written
-// in place: an entry is read and written by one thread, a hole's count and that of the page that moves into it by the
-// hole's.
-__global__ __launch_bounds__(256) void pages_apply_kernel(const BookArgs a)
-{
-    const int32_t *rank = a.scratch + a.nblocks;
-    const int L = a.scratch[a.nblocks + a.P], K = a.count[0];
-    const int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
-    for (int64_t i = i0; i < (int64_t)a.S * a.M; i += step) {
-        const int64_t s = i / a.M, at = s * a.stride + (i - s * a.M);
-        int id = a.table_in[at];
-        // (a page that a table names and whose count is 0 goes nowhere: the entry stays)
-        if (id >= L && id < a.P && rank[id] >= 0) id = a.moves[2 * rank[id] + 1];
-        a.table[at] = id;
-    }
-    for (int64_t i = i0; i < a.P; i += step) {
-        const int id = (int)i, n = a.refs_in[id];
-        if (id < L) {
-            if (n > 0) a.refs[id] = n;
-            else {
-                const int from = a.moves[2 * rank[id]];
-                const int m = a.refs_in[from];
-                a.refs[id] = m;
-                a.refs[from] = 0;
-            }
-        } else if (n <= 0) a.refs[id] = 0;
-        if (id >= K && id < a.P / 2) a.moves[2 * id] = a.moves[2 * id + 1] = -1;
+    if (a.alone) {
+        __syncthreads();         // (what this workgroup has written it sees)
+        apply_moves(a, tid, 1024);
     }
 }
 
