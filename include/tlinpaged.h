@@ -65,7 +65,7 @@ tlin_status tlin_rope_frequencies(int32_t rot, double base, int32_t scaling, dou
                                   double fast, double *freqs, double *amplitude);
 
 typedef struct {
-    int32_t S, T;         /* sequences, new rows of all of them together; each >= 1, T at most 2^30 */
+    int32_t S, T;         /* sequences (at most 65536), new rows of all of them together (at most 2^30); each >= 1 */
     int32_t H, HK;        /* query heads, key heads; HK divides H, at most 64 query heads to a key head */
     int32_t D;            /* head dimension: a multiple of 4 in [8, 128] */
     int32_t page_rows;    /* rows of a page: a power of two in [16, 65536] */
@@ -110,13 +110,14 @@ typedef struct {
     int32_t table_stride;                         /* 0 = table_width */
 } tlin_book_params;
 
-/* Every listed sequence gives up its pages: refs of each one less, its table row -1, its length 0.  seqs int32 [n].  A
+/* Every listed sequence gives up its pages: refs of each one less, its table row -1, its length 0.  seqs int32 [n], n
+ * at most 65536.  A
  * sequence listed twice is freed once; ids outside [0, S) are passed over. */
 tlin_status tlin_pages_free(const tlin_book_params *p, int32_t *table, int32_t *lens, int32_t *refs, const int32_t *seqs,
                             int32_t n, void *stream);
 
 /* Sequence children[i] becomes a copy of sequence parents[i]: it names the same pages (refs of each one more) and has
- * the same length.  status int32 [n]: 0, or 1 where the pair was passed over: an id outside [0, S), a child that holds
+ * the same length.  n at most 65536.  status int32 [n]: 0, or 1 where the pair was passed over: an id outside [0, S), a child that holds
  * rows, that an earlier pair names as a child, or that any pair names as a parent. */
 tlin_status tlin_pages_fork(const tlin_book_params *p, int32_t *table, int32_t *lens, int32_t *refs,
                             const int32_t *parents, const int32_t *children, int32_t n, int32_t *status, void *stream);

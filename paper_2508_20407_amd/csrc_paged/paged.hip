@@ -69,11 +69,13 @@ tlin_status check_rope(const tlin_rope_params *p)
 }
 
 // ---- sizes that the paged calls share
+// (kernels walk over all sequences, free and fork over pairs of them: a bound on how long that takes)
+constexpr int kMaxSequences = 1 << 16;
 tlin_status check_paged(const tlin_paged_params *p)
 {
     if (!p) return TLIN_ERR_INVALID_ARG;
     if (p->S < 1 || p->T < 1 || p->H < 1 || p->HK < 1 || p->T > kMaxRows) return TLIN_ERR_INVALID_ARG;
-    if (p->H % p->HK || p->H / p->HK > 64 || p->H > 1 << 20 || p->S > 1 << 24) return TLIN_ERR_INVALID_ARG;
+    if (p->H % p->HK || p->H / p->HK > 64 || p->H > 1 << 20 || p->S > kMaxSequences) return TLIN_ERR_INVALID_ARG;
     if (!good_dim(p->D)) return TLIN_ERR_UNSUPPORTED;
     if (!good_page_rows(p->page_rows)) return TLIN_ERR_UNSUPPORTED;
     if (p->table_width < 1 || p->num_pages < 1 || (int64_t)p->table_width * p->page_rows > kMaxRows) return TLIN_ERR_INVALID_ARG;
@@ -92,7 +94,7 @@ tlin_status check_paged(const tlin_paged_params *p)
 
 tlin_status check_book(const tlin_book_params *p)
 {
-    if (!p || p->S < 1 || p->S > 1 << 24 || p->table_width < 1 || p->num_pages < 1 || p->num_pages > kMaxRows) return TLIN_ERR_INVALID_ARG;
+    if (!p || p->S < 1 || p->S > kMaxSequences || p->table_width < 1 || p->num_pages < 1 || p->num_pages > kMaxRows) return TLIN_ERR_INVALID_ARG;
     if (!good_page_rows(p->page_rows)) return TLIN_ERR_UNSUPPORTED;
     if ((int64_t)p->table_width * p->page_rows > kMaxRows) return TLIN_ERR_INVALID_ARG;
     if (p->table_stride != 0 && p->table_stride < p->table_width) return TLIN_ERR_INVALID_ARG;
@@ -385,7 +387,8 @@ tlin_status tlin_pages_free(const tlin_book_params *p, int32_t *table, int32_t *
 {
     tlin_status st = check_book(p);
     if (st) return st;
-    if (n < 0 || n > 1 << 24 || !table || !lens || !refs || (n > 0 && !seqs)) return TLIN_ERR_INVALID_ARG;
+    if (n < 0 || n > kMaxSequences || !table || !lens || !refs || (n > 0 && !seqs)) return TLIN_ERR_INVALID_ARG;
+    if (!aligned(table, 4) || !aligned(lens, 4) || !aligned(refs, 4) || !aligned(seqs, 4)) return TLIN_ERR_INVALID_ARG;
     if (n == 0) return TLIN_OK;
     if ((st = check_device())) return st;
     BookArgs a = book_args(p);
@@ -398,7 +401,8 @@ tlin_status tlin_pages_fork(const tlin_book_params *p, int32_t *table, int32_t *
 {
     tlin_status st = check_book(p);
     if (st) return st;
-    if (n < 0 || n > 1 << 24 || !table || !lens || !refs || (n > 0 && (!parents || !children || !status))) return TLIN_ERR_INVALID_ARG;
+    if (n < 0 || n > kMaxSequences || !table || !lens || !refs || (n > 0 && (!parents || !children || !status))) return TLIN_ERR_INVALID_ARG;
+    if (!aligned(table, 4) || !aligned(lens, 4) || !aligned(refs, 4) || !aligned(parents, 4) || !aligned(children, 4) || !aligned(status, 4)) return TLIN_ERR_INVALID_ARG;
     if (n == 0) return TLIN_OK;
     if ((st = check_device())) return st;
     BookArgs a = book_args(p);
@@ -420,6 +424,7 @@ tlin_status tlin_pages_reserve(const tlin_book_params *p, int32_t *table, int32_
     tlin_status st = check_book(p);
     if (st) return st;
     if (!table || !lens || !refs || !want || !moves || !count || !status) return TLIN_ERR_INVALID_ARG;
+    if (!aligned(table, 4) || !aligned(lens, 4) || !aligned(refs, 4) || !aligned(want, 4) || !aligned(moves, 4) || !aligned(count, 4) || !aligned(status, 4)) return TLIN_ERR_INVALID_ARG;
     if (!ws || !aligned(ws, 256) || ws_bytes < tlin_pages_workspace_bytes(p)) return TLIN_ERR_WORKSPACE;
     if ((st = check_device())) return st;
     BookArgs a = book_args(p);
@@ -434,6 +439,7 @@ tlin_status tlin_pages_compact(const tlin_book_params *p, const int32_t *table, 
     tlin_status st = check_book(p);
     if (st) return st;
     if (!table || !refs || !table_out || !refs_out || (!moves && p->num_pages > 1) || !count) return TLIN_ERR_INVALID_ARG;
+    if (!aligned(table, 4) || !aligned(refs, 4) || !aligned(table_out, 4) || !aligned(refs_out, 4) || !aligned(moves, 4) || !aligned(count, 4)) return TLIN_ERR_INVALID_ARG;
     if (!ws || !aligned(ws, 256) || ws_bytes < tlin_pages_workspace_bytes(p)) return TLIN_ERR_WORKSPACE;
     if ((st = check_device())) return st;
     BookArgs a = book_args(p);
@@ -463,6 +469,7 @@ tlin_status tlin_pages_copy(const tlin_cache_params *p, void *a, void *b, const 
     tlin_status st;
     if ((st = check_strides(p->a_stride, p->D, eb))) return st;
     if (b && (st = check_strides(p->b_stride, p->D, eb))) return st;
+    if (!aligned(moves, 4) || !aligned(count, 4)) return TLIN_ERR_INVALID_ARG;
     if (!a || !aligned(a, 16) || !aligned(b, 16) || max_moves < 0 || (max_moves > 0 && !moves)) return TLIN_ERR_INVALID_ARG;
     for (int c = 0; c < (b ? 2 : 1); ++c)
         if (p->layer_stride[c] < 0 || p->layer_stride[c] % (16 / eb)) return TLIN_ERR_INVALID_ARG;

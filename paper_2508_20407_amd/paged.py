@@ -43,10 +43,11 @@ def _refuse(device, dtype, **tensors):
 
 def _ints(name, t, index, size):
     """An int32 vector on the device, at least `size` long."""
+    if t.dtype is _I32 and t.get_device() == index and t.dim() == 1 and t.shape[0] >= size and t.is_contiguous():
+        return
     if t.dtype is not _I32 or t.get_device() != index:
         raise TypeError(f"{name}: an int32 tensor on cuda:{index} expected, not {t.dtype} on {t.device}")
-    if t.dim() != 1 or t.shape[0] < size or (t.shape[0] > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name}: {size} entries, one after another, expected")
+    raise ValueError(f"{name}: {size} entries, one after another, expected")
 
 
 def _rows(t, axes, name):
@@ -57,13 +58,13 @@ def _rows(t, axes, name):
 
 
 def _like(t, dtype=None):
-    """An uninitialised tensor of t's shape, rows of whole 16-byte pieces."""
+    """An uninitialised tensor of t's shape, rows of whole 16-byte pieces (and in t's order, where t is dense)."""
     dt = t.dtype if dtype is None else dtype
     shape = t.shape
     D = shape[-1]
     row = (D + 7) // 8 * 8 if dt is _BF16 else (D + 3) // 4 * 4
     if row == D:
-        return torch.empty(shape, dtype=dt, device=t.device)
+        return torch.empty_like(t, dtype=dt)
     return torch.empty((*shape[:-1], row), dtype=dt, device=t.device)[..., :D]
 
 
@@ -102,6 +103,7 @@ def _call(index, stream, name, *args):
         binding._check(st, name)
 
 
+_ws_bytes = {}     # what the library answered, by the sizes that it goes by
 _scratch = {}      # (device, stream) -> (aligned address, bytes behind it, buffer)
 
 
@@ -112,7 +114,7 @@ def _workspace(device, index, stream, workspace, nbytes):
     if workspace is not None:
         return (*workspace.get(nbytes, device), None)
     have = _scratch.get((index, stream))
-    capturing = torch.cuda.is_current_stream_capturing()
+    capturing = torch._C._cuda_isCurrentStreamCapturing()
     if have is None or have[1] < nbytes or capturing:
         buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
         have = ((buf.data_ptr() + 255) // 256 * 256, nbytes, buf)
@@ -180,16 +182,18 @@ def _table(index, table):
 
 
 def _paged(index, k_pages, v_pages, table, lens, starts, T, H, max_rows, code, out_code, causal, scale, strides):
-    kp, vp = _rows(k_pages, 4, "k_pages"), _rows(v_pages, 4, "v_pages")
-    shape = k_pages.shape
-    if v_pages.shape != shape:
+    kp, vp, shape, entries = k_pages.stride(), v_pages.stride(), k_pages.shape, table.shape
+    if len(kp) != 4 or v_pages.shape != shape or kp[3] != 1 or vp[3] != 1:
+        _rows(k_pages, 4, "k_pages"), _rows(v_pages, 4, "v_pages")
         raise ValueError("k_pages and v_pages must have the same shape")
     P, HK, R, D = shape
-    S, M = _table(index, table)
+    if table.dtype is not _I32 or table.get_device() != index or len(entries) != 2 or (entries[1] > 1 and table.stride(1) != 1):
+        _table(index, table)
+    S, M = entries
     _ints("lens", lens, index, S)
     _ints("starts", starts, index, S + 1)
     return PAGED_LAYOUT.pack(S, T, H, HK, D, R, M, P, T if max_rows is None else min(int(max_rows), T), code, out_code, bool(causal),
-                             scale, table.stride(0) if S > 1 else 0, *strides, *kp, *vp)
+                             scale, table.stride(0) if S > 1 else 0, *strides, kp[0], kp[1], kp[2], vp[0], vp[1], vp[2])
 
 
 def tlin_paged_append(k, v, k_pages, v_pages, table, lens, starts, *, q=None, q_out=None, freqs=None, interleaved=False,
@@ -255,7 +259,13 @@ def tlin_paged_attn(q, k_pages, v_pages, table, lens, starts, *, max_rows=None, 
                D ** -0.5 if scale is None else scale, (*_rows(q, 3, "q"), *_rows(o, 3, "out"), 0, 0, 0, 0))
     lse = torch.empty((H, T), dtype=torch.float32, device=device) if return_lse else None
     stream = _raw_stream(index)
-    ws, nb, _kept = _workspace(device, index, stream, workspace, (_calls or _library()).tlin_paged_workspace_bytes(p))
+    key = (H, k_pages.shape[1], D, code, T if max_rows is None else max_rows if max_rows < T else T)
+    need = _ws_bytes.get(key)
+    if need is None:
+        need = (_calls or _library()).tlin_paged_workspace_bytes(p)
+        if need:
+            _ws_bytes[key] = need
+    ws, nb, _kept = _workspace(device, index, stream, workspace, need)
     _call(index, stream, "tlin_paged_attn", p, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), lens.data_ptr(),
           starts.data_ptr(), o.data_ptr(), lse.data_ptr() if return_lse else None, ws or None, nb)
     return (o, lse) if return_lse else o

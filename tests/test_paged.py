@@ -6,6 +6,9 @@ by n u; bf16 weights by h each and a bf16 result by h once more.
 """
 import ctypes
 import math
+import os
+import re
+import subprocess
 
 import numpy as np
 import pytest
@@ -157,6 +160,42 @@ def test_attention_shared_heads(dtype, G):
 def test_attention_long_sequence_cut_into_many_shares(dtype):
     check_attn(dtype, [9001, 3, 4100], [1, 1, 1], 4, 4, 128, 64, seed=3)
     check_attn(dtype, [9001], [2], 8, 1, 36, 16, seed=4)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("S", [63, 64, 65, 200, 1500])
+def test_attention_many_sequences(dtype, S):
+    """More sequences than lanes: a lane takes a run of them; some without new rows, some without any."""
+    rng = np.random.default_rng(S)
+    lens = rng.integers(0, 60 if S > 200 else 400, S).tolist()
+    check_attn(dtype, lens, [int(n > 0 and rng.random() < 0.8) for n in lens], 2, 1, 64, 16, seed=S)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_calls_on_a_cache_beyond_32_bit_offsets(dtype):
+    """Pages on both sides of 4 GiB: append, copy and attention agree with the same calls on a small cache."""
+    dt, HK, R, D = DT[dtype], 8, 64, 128
+    size = HK * R * D * dt.itemsize
+    P = (1 << 32) // size + 40
+    gen = torch.Generator().manual_seed(11)
+    lens, far = [150, 70], torch.tensor([[P - 1, 0, P - 30], [(1 << 32) // size, (1 << 32) // size - 1, -1]], dtype=torch.int32)
+    near = ints([[0, 1, 2], [3, 4, -1]])
+    new = [torch.randn((n, 220, D), generator=gen).to(dt).cuda() for n in (HK, HK, 16)]
+    out = []
+    for table, pages in ((near, 6), (far, P)):
+        kp, vp = (torch.empty((pages, HK, R, D), dtype=dt, device="cuda") for _ in range(2))
+        last = pages - 2 if pages == P else 5
+        args = (kp, vp, table.cuda(), ints(lens).cuda(), ints([0, 150, 220]).cuda())
+        tl.tlin_paged_append(new[0], new[1], *args)
+        o = tl.tlin_paged_attn(new[2], *args, max_rows=150)
+        step = tl.tlin_paged_attn(new[2][:, :2], *args[:4], ints([0, 1, 2]).cuda(), max_rows=1)
+        tl.tlin_pages_copy(kp, vp, ints([[table[0, 0].item(), last]]).cuda())
+        out.append((o, step, kp[last].clone(), vp[last].clone()))
+        del kp, vp, args
+    for x, y in zip(*out):
+        assert torch.equal(x, y)
 
 
 @gpu
@@ -383,8 +422,6 @@ def test_rope_many_tokens_and_heads_that_share_a_workgroup():
 
 
 def test_rope_frequencies():
-    if not torch.cuda.is_available():
-        pass
     f, a = tl.rope_frequencies(8, 10000.0, device="cpu")
     assert a == 1.0 and torch.allclose(f, 10000.0 ** (-torch.arange(4, dtype=torch.float64) / 4), rtol=1e-15)
     g, a = tl.rope_frequencies(8, 10000.0, scaling="linear", factor=4.0, device="cpu")
@@ -676,7 +713,8 @@ A = 1 << 20      # an aligned address that nothing may follow before it is refus
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(S=0), 1), (dict(T=0), 1), (dict(T=(1 << 30) + 1), 1), (dict(H=0), 1), (dict(HK=0), 1), (dict(HK=3), 1), (dict(H=130, HK=2), 1),
+    (dict(S=0), 1), (dict(S=65537), 1), (dict(T=0), 1), (dict(T=(1 << 30) + 1), 1), (dict(H=0), 1), (dict(kp_stride=(1 << 31, 64, 64)), 1),
+    (dict(vp_stride=(0, 0, 1 << 23), page_rows=1024), 1), (dict(page_rows=65536, HK=512, H=512, table_width=2), 1), (dict(HK=0), 1), (dict(HK=3), 1), (dict(H=130, HK=2), 1),
     (dict(D=4), 2), (dict(D=132), 2), (dict(D=66), 2), (dict(page_rows=8), 2), (dict(page_rows=48), 2), (dict(page_rows=1 << 17), 2),
     (dict(table_width=0), 1), (dict(table_width=1 << 27), 1), (dict(num_pages=0), 1), (dict(max_rows=0), 1), (dict(max_rows=5), 1),
     (dict(dtype=2), 1), (dict(out_dtype=-1), 1), (dict(scale=0.0), 1), (dict(scale=math.nan), 1), (dict(scale=math.inf), 1),
@@ -747,6 +785,10 @@ def test_pages_refusals():
     assert L.tlin_pages_free(p, A, A, A, None, 1, None) == 1 and L.tlin_pages_free(p, A, A, A, A, -1, None) == 1
     assert L.tlin_pages_free(p, A, A, A, None, 0, None) == 0 and L.tlin_pages_fork(p, A, A, A, None, None, 0, None, None) == 0
     assert L.tlin_pages_fork(p, A, A, A, A, A, 1, None, None) == 1
+    assert L.tlin_pages_free(p, A, A, A, A, 65537, None) == 1 and L.tlin_pages_fork(p, A, A, A, A, A, 65537, A, None) == 1
+    for i in range(3):
+        assert L.tlin_pages_free(p, *(A + 2 * (i == k) for k in range(4)), 1, None) == 1
+        assert L.tlin_pages_compact(p, *(A + 2 * (i == k) for k in range(6)), A, need, None) == 1
     assert L.tlin_pages_reserve(p, A, A, A, A, A, A, A, A, need - 1, None) == 3 and L.tlin_pages_reserve(p, A, A, A, A, A, A, A, None, need, None) == 3
     assert L.tlin_pages_compact(p, A, A, A, A, None, A, A, need, None) == 1 and L.tlin_pages_compact(p, A, A, A, A, A, A, A + 4, need, None) == 3
     cache_p = lambda **kw: b.packed(b.TlinCacheParams, b.CACHE_LAYOUT, *dict(dict(layers=1, num_pages=9, HK=2, page_rows=16, D=64, dtype=1), **kw).values(), *(0,) * 8)  # noqa: E731
@@ -754,6 +796,26 @@ def test_pages_refusals():
         assert L.tlin_pages_copy(cache_p(**kw), A, A, A, None, 1, None) == status
     assert L.tlin_pages_copy(cache_p(), None, A, A, None, 1, None) == 1 and L.tlin_pages_copy(cache_p(), A, A + 8, A, None, 1, None) == 1
     assert L.tlin_pages_copy(cache_p(), A, A, None, None, 1, None) == 1 and L.tlin_pages_copy(cache_p(), A, None, None, None, 0, None) == 0
+
+
+LLVM = "/opt/rocm/llvm/bin"
+
+
+@pytest.mark.skipif(not all(os.path.exists(f"{LLVM}/{x}") for x in ("llvm-objcopy", "clang-offload-bundler", "llvm-readelf")), reason="ROCm's LLVM tools not found")
+def test_no_kernel_of_the_paged_cache_spills_registers(tmp_path):
+    fat = tmp_path / "fat"
+    subprocess.run([f"{LLVM}/llvm-objcopy", "-O", "binary", "--only-section=.hip_fatbin", b.LIB_PATH, str(fat)], check=True)
+    data, magic, kernels = fat.read_bytes(), "__CLANG_OFFLOAD_BUNDLE__".encode(), {}
+    starts = [m.start() for m in re.finditer(magic, data)]
+    for i, at in enumerate(starts):
+        part, code = tmp_path / f"part{i}", tmp_path / f"code{i}"
+        part.write_bytes(data[at:starts[i + 1] if i + 1 < len(starts) else None])
+        subprocess.run([f"{LLVM}/clang-offload-bundler", "--unbundle", "--type=o", "--targets=hipv4-amdgcn-amd-amdhsa--gfx950",
+                        f"--input={part}", f"--output={code}"], check=True)
+        notes = subprocess.run([f"{LLVM}/llvm-readelf", "--notes", str(code)], capture_output=True, text=True, check=True).stdout
+        kernels.update(re.findall(r"\.name:\s+(_ZN4tlin\S+).*?\.vgpr_spill_count:\s+(\d+)", notes, flags=re.S))
+    mine = {k: int(n) for k, n in kernels.items() if re.search("paged|pages|rope", k)}
+    assert len(mine) > 30 and not any(mine.values()), {k: n for k, n in mine.items() if n}
 
 
 def test_structures_match_the_header():
