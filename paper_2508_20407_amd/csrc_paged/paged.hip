@@ -359,10 +359,12 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
     a.shares = s.shares;
     a.per_share = 1.0 / s.shares;
     a.per_G = 1.0f / a.G;
-    // What starting an item costs (page ids, queries, first tiles, output: 8 to 12 us), in rows of the cache, by which the
-    // time of uneven batches is least: 64 sequences of up to 8192 rows, 8 key heads x 128, one row each, 64 / 128 / 256 /
-    // 512: 200 / 190 / 182 / 186 us; 2 prompts of 4096 rows, 8 key heads, eight waves, 128 / 256 / 384 / 512: 194 / 164 / 154 / 155.
-    a.start = s.few ? 64 : s.nw == 8 ? 384 : 256;
+    // What starting an item costs (page ids, queries, first tiles, output: 4 to 8 us), in rows of the cache, by which
+    // the times of uneven batches came out lowest.  bf16: 64 sequences of up to 8192 rows, 8 key heads x 128, one row each, 128 /
+    // 256 / 512: 190 / 182 / 186 us; 2 prompts of 4096 rows, 8 key heads, eight waves, 128 / 256 / 384 / 512: 194 / 164 / 154
+    // / 155.  fp32 rows take longer: 3 windows of up to 250 rows over 9000, 12 heads x 36, 32 / 64 / 128 / 256: 129 / 126 / 130 /
+    // 137; 512 rows over 4096, 32 heads x 128: 337 / 327 / 324 / 355.
+    a.start = s.few ? 64 : !bf ? 96 : s.nw == 8 ? 384 : 256;
     a.causal = p->causal != 0;
     a.out_bf16 = p->out_dtype == TLIN_BF16;
     a.scale = p->scale;
