@@ -22,7 +22,6 @@
 
 namespace tlin {
 
-constexpr int SG_SALU = 0x004;       // sched_group_barrier mask (the others: attn_bf16_pipe.h)
 
 // The lane, computed again from here on.
 __device__ __forceinline__ int lane_again()

@@ -15,7 +15,6 @@
 // Products, weights and sums are fp32, in the order of the keys of a share.
 #pragma once
 #include "attn_bf16.h"
-#include "attn_paged_bf16.h"
 #include "share.h"
 
 namespace tlin {

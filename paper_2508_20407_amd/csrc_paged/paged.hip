@@ -20,44 +20,42 @@ int power_of_two(int n)
     return p;
 }
 
-// Elements that a thread takes of each half of its pairs: whole pieces where the halves are whole pieces, else two
-// elements or one.
-int rope_elements(int rot, bool interleaved, int eb)
+// Halves of whole 128-byte lines: a thread takes both pieces of its pairs.  Others go through LDS, a thread a piece of the
+// row (4 x 32 heads x 8192 rows, rotated columns of D: 80 of 80 85 -> 80 us, 64 of 96 95 -> 83, and against threads that take
+// pairs of 4 bytes 100 of 128 242 -> 100, 100 of 100 145 -> 102; 131072 rows, 128 of 128: 407 by halves, 409 to 423 through LDS).
+RopeLayout rope_layout(int rot, bool interleaved, int eb)
 {
-    const int per16 = 16 / eb, half = rot / 2;
-    if (interleaved || half % per16 == 0) return per16;
-    return half % 2 == 0 ? 2 : 1;
+    return interleaved ? ROPE_NEIGHBOURS : rot / 2 * eb % 128 == 0 ? ROPE_HALVES : ROPE_STAGED;
 }
 
-// Lanes of a rotated row (a power of two, the units of the row or more) and tokens of a workgroup: as many as give
-// each thread about four pieces, but a thousand workgroups where there are tokens for them (a hundred tokens would
-// otherwise sit on a few compute units), and few enough that r / H is exact in fp32.
-void rope_shape(RopeArgs &a, int E, bool interleaved, int heads)
+// Lanes of a rotated row (a power of two, the units of the row or more: a row is one wave's) and tokens of a workgroup: as
+// many as give each thread about four pieces (eight where it takes one at a time: append of 9000 rows, 32 + 8 + 8 heads x 128, 100
+// columns 64 -> 53 us), but a thousand workgroups where there are tokens for them (a hundred tokens would otherwise sit on a
+// few compute units), and few enough that r / H is exact in fp32.
+void rope_shape(RopeArgs &a, RopeLayout layout, int eb, int heads)
 {
-    const int units = interleaved ? (a.D + E - 1) / E : a.rot / 2 / E + (a.D - a.rot + E - 1) / E;
-    a.lanes = power_of_two(units);
+    const int E = 16 / eb;
+    a.lanes = power_of_two(layout == ROPE_HALVES ? a.rot / 2 / E + (a.D - a.rot + E - 1) / E : (a.D + E - 1) / E);
     const int64_t work = (int64_t)heads * a.lanes;
-    int64_t tb = 1024 / work;
+    int64_t tb = (layout == ROPE_HALVES ? 1024 : 2048) / work;
     if (tb > a.tokens / 1024) tb = a.tokens / 1024;
     if (tb > kRopeTokens) tb = kRopeTokens;
     a.TB = tb < 1 ? 1 : (int)tb;
 }
 
 template <typename T, bool APPEND>
-const void *rope_kernel_for(int E, bool interleaved)
+const void *rope_kernel_for(RopeLayout layout)
 {
-    constexpr int EP = 16 / sizeof(T);
-    if (interleaved) return (const void *)rope_kernel<T, EP, true, APPEND>;
-    return E == EP ? (const void *)rope_kernel<T, EP, false, APPEND>
-           : E == 2 ? (const void *)rope_kernel<T, 2, false, APPEND> : (const void *)rope_kernel<T, 1, false, APPEND>;
+    return layout == ROPE_HALVES ? (const void *)rope_kernel<T, ROPE_HALVES, APPEND>
+           : layout == ROPE_NEIGHBOURS ? (const void *)rope_kernel<T, ROPE_NEIGHBOURS, APPEND> : (const void *)rope_kernel<T, ROPE_STAGED, APPEND>;
 }
 
 template <bool APPEND>
-tlin_status launch_rope(const RopeArgs &a, int dtype, int E, bool interleaved, hipStream_t st)
+tlin_status launch_rope(const RopeArgs &a, int dtype, RopeLayout layout, hipStream_t st)
 {
     tlin_status s = check_device();
     if (s) return s;
-    const void *kernel = dtype == TLIN_F32 ? rope_kernel_for<float, APPEND>(E, interleaved) : rope_kernel_for<__bf16, APPEND>(E, interleaved);
+    const void *kernel = dtype == TLIN_F32 ? rope_kernel_for<float, APPEND>(layout) : rope_kernel_for<__bf16, APPEND>(layout);
     return launch_kernel(kernel, dim3((a.tokens + a.TB - 1) / a.TB), dim3(256), 0, st, a);
 }
 
@@ -225,9 +223,9 @@ tlin_status tlin_rope(const tlin_rope_params *p, const void *x, void *y, const i
     a.rows = p->rows; a.tokens = p->B * p->rows;
     a.D = p->D; a.rot = p->rot; a.amplitude = p->amplitude; a.negate = p->transpose != 0;
     a.freqs = freqs;
-    const int E = rope_elements(p->rot, p->interleaved, eb);
-    rope_shape(a, E, p->interleaved, p->H);
-    return launch_rope<false>(a, p->dtype, E, p->interleaved != 0, (hipStream_t)stream);
+    const RopeLayout layout = rope_layout(p->rot, p->interleaved != 0, eb);
+    rope_shape(a, layout, eb, p->H);
+    return launch_rope<false>(a, p->dtype, layout, (hipStream_t)stream);
 }
 
 tlin_status tlin_rope_frequencies(int32_t rot, double base, int32_t scaling, double factor, double trained, double slow,
@@ -303,9 +301,9 @@ tlin_status tlin_paged_append(const tlin_paged_params *p, const tlin_rope_params
     a.table_stride = p->table_stride ? p->table_stride : p->table_width;
     a.tokens = p->T;
     a.vlanes = power_of_two(row_elements(p->D, eb) * eb / 16);
-    const int E = rope_elements(a.rot, inter, eb);
-    rope_shape(a, E, inter, (q ? p->H : 0) + 2 * p->HK);
-    return launch_rope<true>(a, p->dtype, E, inter, (hipStream_t)stream);
+    const RopeLayout layout = rope_layout(a.rot, inter, eb);
+    rope_shape(a, layout, eb, (q ? p->H : 0) + 2 * p->HK);
+    return launch_rope<true>(a, p->dtype, layout, (hipStream_t)stream);
 }
 
 size_t tlin_paged_workspace_bytes(const tlin_paged_params *p)

@@ -6,10 +6,12 @@
 // position of 2^20 keeps all digits of its angle), sine and cosine taken in 64 bits and rounded to fp32 once; the
 // turn itself is fp32, rounded to the rows' type once at the end.
 //
-// Bound by HBM: every row is read once and written once.  A workgroup takes TB tokens with all their heads, so
-// that the sines of a token are computed once for all heads that share them (64 pairs: one per thread for four
-// tokens) and kept in LDS; a thread then moves 16-byte pieces.  In the halves layout a thread takes both pieces
-// of its pairs.
+// Bound by HBM: every row is read once and written once.  A workgroup takes TB tokens with all their heads, so that the
+// sines of a token are computed once for all heads (64 pairs: one per thread for four tokens) and kept in LDS; a thread then
+// moves 16-byte pieces: both pieces of its pairs where the halves are whole 128-byte lines, else one piece of the row,
+// whose columns' partners it finds in LDS, where the lanes of the row leave their pieces.  Loads are non-temporal (4 x 32 heads x
+// 8192 rows x 128: 108 -> 101 us), stores where they are whole lines (131072 rows: 426 -> 407; pieces of lines, 80 columns:
+// 85 -> 131 the other way round).
 #pragma once
 #include "common.h"
 
@@ -42,43 +44,43 @@ struct RopeArgs {
     int64_t kp_sp, kp_sr, vp_sp, vp_sr;   // page and row strides of the caches
 };
 
-template <int N> struct Piece;
-template <> struct Piece<16> { typedef u32x4 type; };
-template <> struct Piece<8> { typedef u32x2 type; };
-template <> struct Piece<4> { typedef unsigned type; };
-template <> struct Piece<2> { typedef unsigned short type; };
-
-template <typename T, int E>
+// 16 bytes of a row
+template <typename T>
 union Pack {
-    typename Piece<E * sizeof(T)>::type raw;
-    T e[E];
+    u32x4 raw;
+    T e[16 / sizeof(T)];
 };
 
 // Stores a piece; of the last piece of a bf16 row whose D is not whole pieces only the half that belongs to it.
-template <typename T, int E>
-__device__ __forceinline__ void store_piece(T *at, const Pack<T, E> &p, int left)
+template <typename T>
+__device__ __forceinline__ void store_piece(T *at, const Pack<T> &p, int left)
 {
-    if constexpr (E * sizeof(T) == 16 && sizeof(T) == 2) {
-        if (left < E) {
-            *(u32x2 *)at = u32x2{p.raw[0], p.raw[1]};      // D is a multiple of 4: half of the piece
-            return;
-        }
-    }
-    *(typename Piece<E * sizeof(T)>::type *)at = p.raw;
+    if (left * sizeof(T) < 16) *(u32x2 *)at = u32x2{p.raw[0], p.raw[1]};      // D is a multiple of 4: half of the piece
+    else *(u32x4 *)at = p.raw;
 }
+
+// What lanes of a wave have written to LDS is there for its other lanes: LDS serves a wave in order, the compiler has to.
+__device__ __forceinline__ void wave_step()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// How a row is dealt to threads: both pieces of pairs of halves, a piece of neighbours, a piece of halves by way of LDS.
+enum RopeLayout { ROPE_HALVES, ROPE_NEIGHBOURS, ROPE_STAGED };
 
 constexpr int kRopeTokens = 16;      // most tokens of a workgroup
 constexpr int kRopePairs = 64;       // most pairs of a row
 
-// E: elements that a thread takes at a time (of each half of its pairs).  INTER: pairs of neighbours.
-template <typename T, int E, bool INTER, bool APPEND>
+template <typename T, int LAYOUT, bool APPEND>
 __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a)
 {
-    constexpr int EP = 16 / sizeof(T);          // elements of a whole piece
+    constexpr int E = 16 / sizeof(T);           // elements of a piece
     __shared__ float2 cs[kRopeTokens][kRopePairs];
     __shared__ int where[kRopeTokens];          // position
     __shared__ int place[kRopeTokens];          // append: page of the row, or -1
     __shared__ int live[kRopeTokens];
+    __shared__ u32x4 stage[LAYOUT == ROPE_STAGED ? 256 : 1];
 
     const int tid = threadIdx.x;
     const int g0 = blockIdx.x * a.TB;
@@ -125,14 +127,15 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a)
     }
     __syncthreads();
 
-    const int turned = INTER ? (a.D + E - 1) / E : half / E;       // units that hold pairs
-    const int units = INTER ? turned : turned + (a.D - a.rot + E - 1) / E;
+    // units of a rotated row: of halves those that hold pairs and then the rest of the row, else all pieces
+    const int turned = LAYOUT == ROPE_HALVES ? half / E : (a.D + E - 1) / E;
+    const int units = LAYOUT == ROPE_HALVES ? turned + (a.D - a.rot + E - 1) / E : turned;
 
     // one unit of a rotated row
     auto turn = [&](const T *x, T *y, int t, int u) __attribute__((always_inline)) {
-        if (INTER) {
-            Pack<T, E> p;
-            p.raw = *(const typename Piece<E * sizeof(T)>::type *)(x + u * E);
+        if (LAYOUT == ROPE_NEIGHBOURS) {
+            Pack<T> p;
+            p.raw = __builtin_nontemporal_load((const u32x4 *)(x + u * E));
 #pragma unroll
             for (int e = 0; e < E; e += 2)
                 if (u * E + e < a.rot) {
@@ -141,11 +144,44 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a)
                     p.e[e] = (T)(x1 * w.x - x2 * w.y);
                     p.e[e + 1] = (T)(x1 * w.y + x2 * w.x);
                 }
-            store_piece<T, E>(y + u * E, p, a.D - u * E);
+            store_piece(y + u * E, p, a.D - u * E);
+        } else if (LAYOUT == ROPE_STAGED) {
+            // columns c below half: x[c] cos - x[c + half] sin; from half to rot: x[c] cos + x[c - half] sin.  The lanes of a
+            // row are lanes of one wave: they pass their pieces on through LDS, and in place all have read before one writes.
+            const int c = u * E;
+            Pack<T> p;
+            p.raw = __builtin_nontemporal_load((const u32x4 *)(x + c));
+            stage[tid] = p.raw;
+            wave_step();
+            const T *const row = (const T *)(stage + (tid & ~(a.lanes - 1)));
+            Pack<T> o;
+            if (sizeof(T) == 2 && half % 2 == 0) {             // (uniform) pairs of columns have partners side by side
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    const int at = c + e < half ? c + e + half : c + e - half;
+                    o.raw[e * sizeof(T) / 4] = *(const unsigned *)(row + (c + e < a.rot ? at : 0));
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int at = c + e < half ? c + e + half : c + e - half;
+                    o.e[e] = row[c + e < a.rot ? at : 0];
+                }
+            }
+            wave_step();
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (c + e < a.rot) {
+                    const bool low = c + e < half;
+                    const float2 w = cs[t][low ? c + e : c + e - half];
+                    const float own = (float)p.e[e] * w.x, other = (float)o.e[e] * w.y;
+                    p.e[e] = (T)(low ? own - other : own + other);
+                }
+            store_piece(y + c, p, a.D - c);
         } else if (u < turned) {
-            Pack<T, E> p1, p2;
-            p1.raw = __builtin_nontemporal_load((const typename Piece<E * sizeof(T)>::type *)(x + u * E));
-            p2.raw = __builtin_nontemporal_load((const typename Piece<E * sizeof(T)>::type *)(x + half + u * E));
+            Pack<T> p1, p2;
+            p1.raw = __builtin_nontemporal_load((const u32x4 *)(x + u * E));
+            p2.raw = __builtin_nontemporal_load((const u32x4 *)(x + half + u * E));
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const float2 w = cs[t][u * E + e];
@@ -153,13 +189,13 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a)
                 p1.e[e] = (T)(x1 * w.x - x2 * w.y);
                 p2.e[e] = (T)(x1 * w.y + x2 * w.x);
             }
-            __builtin_nontemporal_store(p1.raw, (typename Piece<E * sizeof(T)>::type *)(y + u * E));
-            __builtin_nontemporal_store(p2.raw, (typename Piece<E * sizeof(T)>::type *)(y + half + u * E));
+            __builtin_nontemporal_store(p1.raw, (u32x4 *)(y + u * E));
+            __builtin_nontemporal_store(p2.raw, (u32x4 *)(y + half + u * E));
         } else {
             const int col = a.rot + (u - turned) * E;
-            Pack<T, E> p;
-            p.raw = *(const typename Piece<E * sizeof(T)>::type *)(x + col);
-            store_piece<T, E>(y + col, p, a.D - col);
+            Pack<T> p;
+            p.raw = __builtin_nontemporal_load((const u32x4 *)(x + col));
+            store_piece(y + col, p, a.D - col);
         }
     };
     // f(token, head, unit) over the rows of these tokens, `lanes` lanes to a row
@@ -195,11 +231,11 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a)
             turn(x, (T *)a.k.y + place[t] * a.kp_sp + h * a.k.y_sh + (where[t] & mask) * a.kp_sr, t, u);
         });
         each(a.v.H, a.vlanes, [&](int t, int h, int u) __attribute__((always_inline)) {
-            if (u * EP >= a.D || !live[t] || place[t] < 0) return;
-            const T *x = (const T *)a.v.x + (int64_t)h * a.v.x_sh + (int64_t)(g0 + t) * a.v.x_sr + u * EP;
-            Pack<T, EP> p;
+            if (u * E >= a.D || !live[t] || place[t] < 0) return;
+            const T *x = (const T *)a.v.x + (int64_t)h * a.v.x_sh + (int64_t)(g0 + t) * a.v.x_sr + u * E;
+            Pack<T> p;
             p.raw = *(const u32x4 *)x;
-            store_piece<T, EP>((T *)a.v.y + place[t] * a.vp_sp + h * a.v.y_sh + (where[t] & mask) * a.vp_sr + u * EP, p, a.D - u * EP);
+            store_piece((T *)a.v.y + place[t] * a.vp_sp + h * a.v.y_sh + (where[t] & mask) * a.vp_sr + u * E, p, a.D - u * E);
         });
     }
 }
