@@ -700,6 +700,104 @@ def test_serving_steps_together():
     assert lens.tolist() == [len(x[0]) for x in hist]
 
 
+@gpu
+def test_a_captured_serving_step():
+    """Reserve, copy, append and attention in one graph, scratch taken by default: every replay is the eager step to the bit,
+    with larger eager calls between."""
+    gen = torch.Generator().manual_seed(14)
+    S, M, P, R, H, HK, D = 5, 12, 50, 16, 4, 2, 64
+    dt = torch.bfloat16
+    freqs = tl.rope_frequencies(D)[0]
+    book = Book(S, M, P, R)
+    start = book.gpu()
+    caches = torch.randn((2, P, HK, R, D), generator=gen).to(dt).cuda()
+    q, k, v = (torch.randn((n, S, D), generator=gen).to(dt).cuda() for n in (H, HK, HK))
+    starts, want = ints(range(S + 1)).cuda(), ints([1] * S).cuda()
+    big = torch.randn((H, 300, D), generator=gen).to(dt).cuda()
+
+    def step(table, lens, refs, kp, vp, out):
+        moves, count, status = tl.tlin_pages_reserve(table, lens, refs, want, R)
+        tl.tlin_pages_copy(kp, vp, moves, count)
+        qr = tl.tlin_paged_append(k, v, kp, vp, table, lens, starts, q=q, freqs=freqs)
+        tl.tlin_paged_attn(qr, kp, vp, table, lens, starts, max_rows=1, out=out)
+        return status
+
+    sides = []
+    for _ in range(2):                       # the eager side, the captured one
+        table, lens, refs = (x.clone() for x in start)
+        kp, vp = caches[0].clone(), caches[1].clone()
+        tl.tlin_pages_reserve(table, lens, refs, ints([30, 1, 0, 47, 16]).cuda(), R)
+        tl.tlin_pages_fork(table, lens, refs, ints([0]).cuda(), ints([2]).cuda(), R)
+        sides.append((table, lens, refs, kp, vp, torch.full((H, S, D), 7.0, dtype=dt).cuda()))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(*sides[1])
+    for turn_ in range(20):
+        status = step(*sides[0])
+        if turn_ % 4 == 1:                   # more scratch than the step's, new memory
+            tl.tlin_paged_attn(big, sides[0][3], sides[0][4], sides[0][0], sides[0][1], ints([0, 60, 120, 180, 240, 300]).cuda())
+        g.replay()
+        torch.cuda.synchronize()
+        assert status.sum().item() == 0
+        for name, a, c in zip(("table", "lens", "refs", "k", "v", "out"), *sides):
+            assert torch.equal(a, c), (turn_, name)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_graphs_captured_one_after_another_run_side_by_side(dtype):
+    """Two graphs captured on one stream without workspaces of their own, replayed on two streams at once."""
+    gen = torch.Generator().manual_seed(15)
+    dt = DT[dtype]
+    k, v, table = (x.cuda() for x in cache(gen, dt, [9000, 40, 3000], 2, 64, 64))
+    lens, starts = ints([9000, 40, 3000]).cuda(), ints([0, 2, 5, 6]).cuda()
+    qs = [torch.randn((4, 6, 64), generator=gen).to(dt).cuda() for _ in range(2)]
+    call = lambda q, o=None: tl.tlin_paged_attn(q, k, v, table, lens, starts, max_rows=3, out=o)  # noqa: E731
+    want = [call(q) for q in qs]
+    outs, graphs, streams = [torch.empty_like(w) for w in want], [torch.cuda.CUDAGraph() for _ in qs], [torch.cuda.Stream() for _ in qs]
+    on = torch.cuda.Stream()
+    for q, o, g in zip(qs, outs, graphs):
+        with torch.cuda.graph(g, stream=on):
+            call(q, o)
+    for step in range(5):
+        for o in outs:
+            o.fill_(7)
+        torch.cuda.synchronize()
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                for _ in range(4):
+                    g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want)), step
+
+
+@gpu
+def test_tables_that_are_columns_of_a_wider_one():
+    gen = torch.Generator().manual_seed(16)
+    lens, R = [100, 1, 33], 16
+    k, v, table = (x.cuda() for x in cache(gen, torch.bfloat16, lens, 2, 64, R))
+    S, M, P = *table.shape, k.shape[0]
+    wide = torch.full((S, M + 5), 12345, dtype=torch.int32).cuda()
+    view = wide[:, 2:2 + M]
+    view.copy_(table)
+    q, kn, vn = (torch.randn((n, 5, 64), generator=gen).to(torch.bfloat16).cuda() for n in (4, 2, 2))
+    refs = torch.bincount(table[table >= 0].long(), minlength=P).to(torch.int32)
+    got = []
+    for t in (table, view):
+        kp, vp, r, ln, starts = k.clone(), v.clone(), refs.clone(), ints(lens).cuda(), ints([0, 2, 3, 5]).cuda()
+        tl.tlin_paged_append(kn, vn, kp, vp, t, ln, starts)
+        o = tl.tlin_paged_attn(q, kp, vp, t, ln, starts, max_rows=2)
+        tl.tlin_pages_free(t, ln, r, ints([1]).cuda())
+        tl.tlin_pages_fork(t, ln, r, ints([2]).cuda(), ints([1]).cuda(), R)
+        moves, count, status = tl.tlin_pages_reserve(t, ln, r, ints([1, 2, 3]).cuda(), R)
+        tl.tlin_pages_copy(kp, vp, moves, count)
+        _, _, m2, c2 = tl.tlin_pages_compact(t, r)
+        got.append((o, ln, r, moves, count, status, m2, c2, t.clone(), torch.nan_to_num(kp), torch.nan_to_num(vp)))
+    for i, (a, c) in enumerate(zip(*got)):
+        assert torch.equal(a, c), i
+    assert (wide[:, :2] == 12345).all() and (wide[:, 2 + M:] == 12345).all()
+
+
 # ---------------------------------------------------------------- refusals, on the host
 def packed_paged(**kw):
     d = dict(S=2, T=4, H=4, HK=2, D=64, page_rows=16, table_width=3, num_pages=9, max_rows=2, dtype=1, out_dtype=1, causal=1,
