@@ -13,29 +13,23 @@ namespace {
 
 // ---- rotary positions and append
 
-int power_of_two(int n)
-{
-    int p = 1;
-    while (p < n) p *= 2;
-    return p;
-}
-
 // Halves of whole 128-byte lines: a thread takes both pieces of its pairs.  Others go through LDS, a thread a piece of the
-// row (4 x 32 heads x 8192 rows, rotated columns of D: 80 of 80 85 -> 80 us, 64 of 96 95 -> 83, and against threads that take
-// pairs of 4 bytes 100 of 128 242 -> 100, 100 of 100 145 -> 102; 131072 rows, 128 of 128: 407 by halves, 409 to 423 through LDS).
+// row (4 x 32 heads x 8192 rows, rotated columns of D, 36 of 36 at 16384: 115 -> 80 us, 80 of 80 85 -> 66, 64 of 96 95 -> 72,
+// and against threads that take pairs of 4 bytes 100 of 128 242 -> 99, 100 of 100 145 -> 92; 131072 rows, 128 of 128: by halves
+// 407 when it was 409 to 423 through LDS).
 RopeLayout rope_layout(int rot, bool interleaved, int eb)
 {
     return interleaved ? ROPE_NEIGHBOURS : rot / 2 * eb % 128 == 0 ? ROPE_HALVES : ROPE_STAGED;
 }
 
-// Lanes of a rotated row (a power of two, the units of the row or more: a row is one wave's) and tokens of a workgroup: as
-// many as give each thread about four pieces (eight where it takes one at a time: append of 9000 rows, 32 + 8 + 8 heads x 128, 100
-// columns 64 -> 53 us), but a thousand workgroups where there are tokens for them (a hundred tokens would otherwise sit on a
-// few compute units), and few enough that r / H is exact in fp32.
+// Lanes of a rotated row (one for each of its units: a row is one wave's) and tokens of a workgroup: as many as give each
+// thread about four pieces (eight where it takes one at a time: append of 9000 rows, 32 + 8 + 8 heads x 128, 100 columns
+// 64 -> 53 us; by halves 46 -> 55), but a thousand workgroups where there are tokens for them (a hundred tokens would
+// otherwise sit on a few compute units), and few enough that the kernel's divisions in fp32 are exact.
 void rope_shape(RopeArgs &a, RopeLayout layout, int eb, int heads)
 {
     const int E = 16 / eb;
-    a.lanes = power_of_two(layout == ROPE_HALVES ? a.rot / 2 / E + (a.D - a.rot + E - 1) / E : (a.D + E - 1) / E);
+    a.lanes = layout == ROPE_HALVES ? a.rot / 2 / E + (a.D - a.rot + E - 1) / E : (a.D + E - 1) / E;
     const int64_t work = (int64_t)heads * a.lanes;
     int64_t tb = (layout == ROPE_HALVES ? 1024 : 2048) / work;
     if (tb > a.tokens / 1024) tb = a.tokens / 1024;
@@ -300,7 +294,7 @@ tlin_status tlin_paged_append(const tlin_paged_params *p, const tlin_rope_params
     a.S = p->S; a.M = p->table_width; a.P = p->num_pages; a.lr = log2_of(p->page_rows);
     a.table_stride = p->table_stride ? p->table_stride : p->table_width;
     a.tokens = p->T;
-    a.vlanes = power_of_two(row_elements(p->D, eb) * eb / 16);
+    a.vlanes = row_elements(p->D, eb) * eb / 16;
     const RopeLayout layout = rope_layout(a.rot, inter, eb);
     rope_shape(a, layout, eb, (q ? p->H : 0) + 2 * p->HK);
     return launch_rope<true>(a, p->dtype, layout, (hipStream_t)stream);

@@ -10,7 +10,7 @@
 // sines of a token are computed once for all heads (64 pairs: one per thread for four tokens) and kept in LDS; a thread then
 // moves 16-byte pieces: both pieces of its pairs where the halves are whole 128-byte lines, else one piece of the row,
 // whose columns' partners it finds in LDS, where the lanes of the row leave their pieces.  Loads are non-temporal (4 x 32 heads x
-// 8192 rows x 128: 108 -> 101 us), stores where they are whole lines (131072 rows: 426 -> 407; pieces of lines, 80 columns:
+// 8192 rows x 128: 108 -> 101 us), stores where a thread's are whole lines' (131072 rows: 426 -> 407; pieces of lines, 80 columns:
 // 85 -> 131 the other way round).
 #pragma once
 #include "common.h"
@@ -32,7 +32,7 @@ struct RopeArgs {
     int32_t rows;            // rows of a batch
     int32_t tokens;          // B * rows, or T
     int32_t TB;              // tokens of a workgroup
-    int32_t lanes, vlanes;   // lanes of a row, powers of two: at least the units of a rotated row, of a copied row
+    int32_t lanes, vlanes;   // lanes of a row: the units of a rotated row, of a copied row
     int32_t D, rot;
     float amplitude;
     int32_t negate;
@@ -127,9 +127,7 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a)
     }
     __syncthreads();
 
-    // units of a rotated row: of halves those that hold pairs and then the rest of the row, else all pieces
-    const int turned = LAYOUT == ROPE_HALVES ? half / E : (a.D + E - 1) / E;
-    const int units = LAYOUT == ROPE_HALVES ? turned + (a.D - a.rot + E - 1) / E : turned;
+    const int turned = half / E;                // ROPE_HALVES: units that hold pairs, the rest of the row behind them
 
     // one unit of a rotated row
     auto turn = [&](const T *x, T *y, int t, int u) __attribute__((always_inline)) {
@@ -153,7 +151,7 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a)
             p.raw = __builtin_nontemporal_load((const u32x4 *)(x + c));
             stage[tid] = p.raw;
             wave_step();
-            const T *const row = (const T *)(stage + (tid & ~(a.lanes - 1)));
+            const T *const row = (const T *)(stage + (tid - u));
             Pack<T> o;
             if (sizeof(T) == 2 && half % 2 == 0) {             // (uniform) pairs of columns have partners side by side
 #pragma unroll
@@ -198,19 +196,23 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a)
             store_piece(y + col, p, a.D - col);
         }
     };
-    // f(token, head, unit) over the rows of these tokens, `lanes` lanes to a row
-    auto each = [&](int H, int lanes, auto f) __attribute__((always_inline)) {
-        const int u = tid & (lanes - 1), step = 256 / lanes;
-        const float inv = 1.0f / (float)H;
-        for (int r = tid / lanes; r < nt * H; r += step) {
-            // r / H: exact where several tokens share a workgroup (r below 2^13, see rope_tokens)
-            const int t = a.TB == 1 ? 0 : (int)(((float)r + 0.5f) * inv);
-            f(t, r - t * H, u);
+    // f(token, head, unit) over the rows of these tokens: as many whole rows to a wave as it has lanes for, rows that follow
+    // each other in memory by following lanes (tokens of a head where `down`: 32 heads of 131072 rows x 128, 407 -> 360 us;
+    // 96 columns, twelve lanes of a row among five rows a wave, 82 -> 72)
+    auto each = [&](int H, int lanes, bool down, auto f) __attribute__((always_inline)) {
+        const int lane = tid & 63, mine = (int)(((float)lane + 0.5f) * (1.0f / (float)lanes)), u = lane - mine * lanes, rows = 64 / lanes;
+        if (mine >= rows) return;
+        const int n = down ? nt : H;
+        const float inv = 1.0f / (float)n;
+        for (int r = (tid >> 6) * rows + mine; r < nt * H; r += 4 * rows) {
+            // r / n: exact, r is below 2^13 where several tokens share a workgroup (rope_shape), else below 2^20
+            const int q = (int)(((float)r + 0.5f) * inv), m = r - q * n;
+            f(down ? m : q, down ? q : m, u);
         }
     };
     if (a.q.x)
-        each(a.q.H, a.lanes, [&](int t, int h, int u) __attribute__((always_inline)) {
-            if (u >= units || (APPEND && !live[t])) return;
+        each(a.q.H, a.lanes, a.q.y_sr < a.q.y_sh, [&](int t, int h, int u) __attribute__((always_inline)) {
+            if (APPEND && !live[t]) return;
             const int g = g0 + t;
             int64_t xo = (int64_t)h * a.q.x_sh, yo = (int64_t)h * a.q.y_sh;
             if (APPEND) {
@@ -225,13 +227,13 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a)
         });
     if (APPEND) {
         const int mask = (1 << a.lr) - 1;
-        each(a.k.H, a.lanes, [&](int t, int h, int u) __attribute__((always_inline)) {
-            if (u >= units || !live[t] || place[t] < 0) return;
+        each(a.k.H, a.lanes, a.kp_sr < a.k.y_sh, [&](int t, int h, int u) __attribute__((always_inline)) {
+            if (!live[t] || place[t] < 0) return;
             const T *x = (const T *)a.k.x + (int64_t)h * a.k.x_sh + (int64_t)(g0 + t) * a.k.x_sr;
             turn(x, (T *)a.k.y + place[t] * a.kp_sp + h * a.k.y_sh + (where[t] & mask) * a.kp_sr, t, u);
         });
-        each(a.v.H, a.vlanes, [&](int t, int h, int u) __attribute__((always_inline)) {
-            if (u * E >= a.D || !live[t] || place[t] < 0) return;
+        each(a.v.H, a.vlanes, a.vp_sr < a.v.y_sh, [&](int t, int h, int u) __attribute__((always_inline)) {
+            if (!live[t] || place[t] < 0) return;
             const T *x = (const T *)a.v.x + (int64_t)h * a.v.x_sh + (int64_t)(g0 + t) * a.v.x_sr + u * E;
             Pack<T> p;
             p.raw = *(const u32x4 *)x;
