@@ -18,6 +18,7 @@
  *   - New rows are ragged: those of sequence s are rows starts[s] .. starts[s+1]-1 of tensors
  *     [heads, T, D], and they are the LAST rows of the sequence, which has lens[s] rows with them: row
  *     starts[s] + i is at position lens[s] - (starts[s+1] - starts[s]) + i.
+ *   - A stride of 0 repeats what is read; a tensor that is written has none on an axis longer than one (refused).
  *   - Key heads may be shared: query head h reads key head h / (H / HK); HK divides H.
  *   - What the device arrays hold cannot be refused by the host, so the kernels check it: lengths are cut to
  *     what the table can name (table_width * page_rows) and starts to [0, T]; a page id outside
@@ -48,7 +49,8 @@ typedef struct {
 /* y = x with pair i of a row at position p turned by the angle p * freqs[i] and multiplied by amplitude:
  *   y1 = a (x1 cos - x2 sin),  y2 = a (x1 sin + x2 cos).
  * pos: int32 [rows] or [B, rows].  freqs: double [rot/2], on the device; angles are reduced in 64 bits, so that
- * positions may be any int32.  y may be x (the same strides), and must not overlap it otherwise. */
+ * positions may be any int32.  y may be x (the same strides), and must not overlap it otherwise.  More rows than a
+ * launch has workgroups for (2^24, of 1 to 16 rows with all heads) are TLIN_ERR_UNSUPPORTED. */
 tlin_status tlin_rope(const tlin_rope_params *p, const void *x, void *y, const int32_t *pos, const double *freqs, void *stream);
 
 /* Frequencies for tlin_rope, host arithmetic only: freqs[i] = base^(-2i/rot), i < rot/2, for

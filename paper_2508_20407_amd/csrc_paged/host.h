@@ -83,6 +83,16 @@ void resolve(const int64_t (&s)[N], const int64_t (&sizes)[N - 1], int D, int64_
     for (int i = N - 2; i >= 0; --i) out[i] = out[i + 1] * sizes[i];
 }
 
+// Whether entries that are written lie on one another: sizes[0] entries along the first axis and so on, the rows' axis left
+// out (check_strides).
+template <int N>
+bool written_twice(const int64_t (&s)[N], const int64_t (&sizes)[N - 1])
+{
+    for (int i = 0; i < N - 1; ++i)
+        if (s[i] == 0 && sizes[i] > 1) return true;
+    return false;
+}
+
 inline bool good_dim(int32_t D) { return D >= 8 && D <= 128 && D % 4 == 0; }
 
 }  // namespace

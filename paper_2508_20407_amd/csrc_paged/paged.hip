@@ -47,10 +47,12 @@ const void *rope_kernel_for(RopeLayout layout)
 template <bool APPEND>
 tlin_status launch_rope(const RopeArgs &a, int dtype, RopeLayout layout, hipStream_t st)
 {
+    const int blocks = (a.tokens + a.TB - 1) / a.TB;
+    if (blocks >= 1 << 24) return TLIN_ERR_UNSUPPORTED;       // a launch has fewer than 2^32 threads
     tlin_status s = check_device();
     if (s) return s;
     const void *kernel = dtype == TLIN_F32 ? rope_kernel_for<float, APPEND>(layout) : rope_kernel_for<__bf16, APPEND>(layout);
-    return launch_kernel(kernel, dim3((a.tokens + a.TB - 1) / a.TB), dim3(256), 0, st, a);
+    return launch_kernel(kernel, dim3(blocks), dim3(256), 0, st, a);
 }
 
 tlin_status check_rope(const tlin_rope_params *p)
@@ -207,9 +209,10 @@ tlin_status tlin_rope(const tlin_rope_params *p, const void *x, void *y, const i
     if (!aligned(x, 16) || !aligned(y, 16) || !aligned(pos, 4) || !aligned(freqs, 8)) return TLIN_ERR_INVALID_ARG;
     RopeArgs a = {};
     int64_t xs[3], ys[3];
-    const int64_t sizes[2] = {p->H, p->rows};
+    const int64_t sizes[2] = {p->H, p->rows}, outer[2] = {p->B, p->H};
     resolve(p->x_stride, sizes, p->D, xs);
     resolve(p->y_stride, sizes, p->D, ys);
+    if (written_twice(ys, outer)) return TLIN_ERR_INVALID_ARG;
     if (x == y && (xs[0] != ys[0] || xs[1] != ys[1] || xs[2] != ys[2])) return TLIN_ERR_INVALID_ARG;
     a.q = {x, y, xs[1], xs[2], ys[1], ys[2], p->H};
     a.q_sb = xs[0]; a.qy_sb = ys[0];
@@ -263,7 +266,7 @@ tlin_status tlin_paged_append(const tlin_paged_params *p, const tlin_rope_params
     bool inter = true;       // nothing is rotated: whole pieces, none of which holds pairs
     a.D = p->D;
     int64_t s1[2], s2[2], s3[3];
-    const int64_t rows[1] = {p->T}, page[2] = {p->HK, p->page_rows};
+    const int64_t rows[1] = {p->T}, page[2] = {p->HK, p->page_rows}, heads[1] = {p->H}, outer[2] = {p->num_pages, p->HK};
     if (r) {
         tlin_rope_params c = *r;
         c.D = p->D;
@@ -276,6 +279,7 @@ tlin_status tlin_paged_append(const tlin_paged_params *p, const tlin_rope_params
             if (!aligned(q, 16) || !aligned(q_out, 16)) return TLIN_ERR_INVALID_ARG;
             resolve(p->q_stride, rows, p->D, s1);
             resolve(p->o_stride, rows, p->D, s2);
+            if (written_twice(s2, heads)) return TLIN_ERR_INVALID_ARG;
             if (q == q_out && (s1[0] != s2[0] || s1[1] != s2[1])) return TLIN_ERR_INVALID_ARG;
             a.q = {q, q_out, s1[0], s1[1], s2[0], s2[1], p->H};
         }
@@ -284,10 +288,12 @@ tlin_status tlin_paged_append(const tlin_paged_params *p, const tlin_rope_params
     }
     resolve(p->k_stride, rows, p->D, s1);
     resolve(p->kp_stride, page, p->D, s3);
+    if (written_twice(s3, outer)) return TLIN_ERR_INVALID_ARG;
     a.k = {k, k_pages, s1[0], s1[1], s3[1], 0, p->HK};
     a.kp_sp = s3[0]; a.kp_sr = s3[2];
     resolve(p->v_stride, rows, p->D, s1);
     resolve(p->vp_stride, page, p->D, s3);
+    if (written_twice(s3, outer)) return TLIN_ERR_INVALID_ARG;
     a.v = {v, v_pages, s1[0], s1[1], s3[1], 0, p->HK};
     a.vp_sp = s3[0]; a.vp_sr = s3[2];
     a.table = table; a.lens = lens; a.starts = starts;
@@ -319,6 +325,10 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
     if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(O, 16)) return TLIN_ERR_INVALID_ARG;
     if (!aligned(table, 4) || !aligned(lens, 4) || !aligned(starts, 4) || !aligned(lse, 4)) return TLIN_ERR_INVALID_ARG;
     if (!ws || !aligned(ws, 256) || ws_bytes < tlin_paged_workspace_bytes(p)) return TLIN_ERR_WORKSPACE;
+    int64_t s2[2], s3[3];
+    const int64_t rows[1] = {p->T}, page[2] = {p->HK, p->page_rows}, heads[1] = {p->H};
+    resolve(p->o_stride, rows, p->D, s2);
+    if (written_twice(s2, heads)) return TLIN_ERR_INVALID_ARG;
     if ((st = check_device())) return st;
 
     const PagedShape s = paged_shape(p);
@@ -326,16 +336,13 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
     PagedArgs a = {};
     PagedWorkspace w;
     paged_workspace(s, ws, w);
-    int64_t s2[2], s3[3];
-    const int64_t rows[1] = {p->T}, page[2] = {p->HK, p->page_rows};
     a.Q = q; a.K = k_pages; a.V = v_pages;
     a.table = table; a.lens = lens; a.starts = starts;
     a.O = O; a.lse = lse;
     a.Opart = w.O; a.Mpart = w.M; a.Lpart = w.L; a.cuts = w.cuts;
+    a.o_sh = s2[0]; a.o_sr = s2[1];
     resolve(p->q_stride, rows, p->D, s2);
     a.q_sh = s2[0]; a.q_sr = s2[1];
-    resolve(p->o_stride, rows, p->D, s2);
-    a.o_sh = s2[0]; a.o_sr = s2[1];
     resolve(p->kp_stride, page, p->D, s3);
     a.k_sp = s3[0]; a.k_sh = s3[1]; a.k_sr = s3[2];
     resolve(p->vp_stride, page, p->D, s3);
@@ -465,8 +472,14 @@ tlin_status tlin_pages_copy(const tlin_cache_params *p, void *a, void *b, const 
     if (b && (st = check_strides(p->b_stride, p->D, eb))) return st;
     if (!aligned(moves, 4) || !aligned(count, 4)) return TLIN_ERR_INVALID_ARG;
     if (!a || !aligned(a, 16) || !aligned(b, 16) || max_moves < 0 || (max_moves > 0 && !moves)) return TLIN_ERR_INVALID_ARG;
-    for (int c = 0; c < (b ? 2 : 1); ++c)
+    const int64_t sizes[2] = {p->HK, p->page_rows}, outer[2] = {p->num_pages, p->HK};
+    int64_t strides[2][3];
+    resolve(p->a_stride, sizes, p->D, strides[0]);
+    resolve(p->b_stride, sizes, p->D, strides[1]);
+    for (int c = 0; c < (b ? 2 : 1); ++c) {
         if (p->layer_stride[c] < 0 || p->layer_stride[c] % (16 / eb)) return TLIN_ERR_INVALID_ARG;
+        if (written_twice(strides[c], outer)) return TLIN_ERR_INVALID_ARG;
+    }
     if (max_moves == 0) return TLIN_OK;
     if ((st = check_device())) return st;
     CopyArgs g = {};
@@ -476,11 +489,8 @@ tlin_status tlin_pages_copy(const tlin_cache_params *p, void *a, void *b, const 
     const int re = row_elements(p->D, eb);
     g.row_pieces = re * eb / 16;
     g.pieces = (int64_t)p->HK * p->page_rows * g.row_pieces;
-    const int64_t sizes[2] = {p->HK, p->page_rows};
     for (int c = 0; c < g.caches; ++c) {
-        int64_t s[3];
-        if (c == 0) resolve(p->a_stride, sizes, p->D, s);
-        else resolve(p->b_stride, sizes, p->D, s);
+        const int64_t(&s)[3] = strides[c];
         g.cache[c] = (char *)(c == 0 ? a : b);
         g.layer[c] = (p->layer_stride[c] ? p->layer_stride[c] : s[0] * p->num_pages) * eb;
         g.page[c] = s[0] * eb; g.head[c] = s[1] * eb; g.row[c] = s[2] * eb;

@@ -54,7 +54,18 @@ def _rows(t, axes, name):
     st = t.stride()
     if len(st) != axes or (st[-1] != 1 and t.shape[-1] != 1):
         raise ValueError(f"{name}: {axes} axes expected, the last one contiguous")
+    if not st[-2]:           # (strides of zeros alone would be taken for those of a dense tensor)
+        if t.shape[-2] > 1:
+            raise ValueError(f"{name}: rows that lie on one another")
+        return (*st[:-2], (t.shape[-1] + 7) // 8 * 8)
     return st[:-1]
+
+
+def _table_stride(table, S):
+    st = table.stride(0) if S > 1 else 0
+    if S > 1 and not st:
+        raise ValueError("table: rows that lie on one another")
+    return st
 
 
 def _like(t, dtype=None):
@@ -183,7 +194,7 @@ def _table(index, table):
 
 def _paged(index, k_pages, v_pages, table, lens, starts, T, H, max_rows, code, out_code, causal, scale, strides):
     kp, vp, shape, entries = k_pages.stride(), v_pages.stride(), k_pages.shape, table.shape
-    if len(kp) != 4 or v_pages.shape != shape or kp[3] != 1 or vp[3] != 1:
+    if len(kp) != 4 or v_pages.shape != shape or kp[3] != 1 or vp[3] != 1 or not (kp[2] and vp[2]):
         _rows(k_pages, 4, "k_pages"), _rows(v_pages, 4, "v_pages")
         raise ValueError("k_pages and v_pages must have the same shape")
     P, HK, R, D = shape
@@ -193,7 +204,7 @@ def _paged(index, k_pages, v_pages, table, lens, starts, T, H, max_rows, code, o
     _ints("lens", lens, index, S)
     _ints("starts", starts, index, S + 1)
     return PAGED_LAYOUT.pack(S, T, H, HK, D, R, M, P, T if max_rows is None else min(int(max_rows), T), code, out_code, bool(causal),
-                             scale, table.stride(0) if S > 1 else 0, *strides, kp[0], kp[1], kp[2], vp[0], vp[1], vp[2])
+                             scale, _table_stride(table, S), *strides, kp[0], kp[1], kp[2], vp[0], vp[1], vp[2])
 
 
 def tlin_paged_append(k, v, k_pages, v_pages, table, lens, starts, *, q=None, q_out=None, freqs=None, interleaved=False,
@@ -279,7 +290,7 @@ def _book(table, refs, page_rows):
         _refuse(table.device, None, table=table)
     S, M = _table(index, table)
     _ints("refs", refs, index, 1)
-    return BOOK_LAYOUT.pack(S, M, refs.shape[0], int(page_rows), table.stride(0) if S > 1 else 0), S, index
+    return BOOK_LAYOUT.pack(S, M, refs.shape[0], int(page_rows), _table_stride(table, S)), S, index
 
 
 def tlin_pages_free(table, lens, refs, seqs, page_rows=16):
@@ -362,6 +373,8 @@ def tlin_pages_copy(k_pages, v_pages, moves, count=None):
     ks = _rows(k_pages, axes, "k_pages")
     vs = _rows(v_pages, axes, "v_pages") if v_pages is not None else (0,) * (axes - 1)
     L, kl, vl = (shape[0], ks[0], vs[0]) if axes == 5 else (1, 0, 0)
+    if L > 1 and not (kl and (vl or v_pages is None)):
+        raise ValueError("layers that lie on one another")
     p = CACHE_LAYOUT.pack(L, *shape[-4:], _code(dt), kl, vl, *ks[-3:], *vs[-3:])
     _call(index, _raw_stream(index), "tlin_pages_copy", p, k_pages.data_ptr(), None if v_pages is None else v_pages.data_ptr(),
           moves.data_ptr(), None if count is None else count.data_ptr(), moves.shape[0])

@@ -916,6 +916,63 @@ def test_no_kernel_of_the_paged_cache_spills_registers(tmp_path):
     assert len(mine) > 30 and not any(mine.values()), {k: n for k, n in mine.items() if n}
 
 
+def test_refusals_of_what_would_be_written_twice():
+    """A stride of 0 on an axis of more than one entry, in tensors that are written."""
+    L = b.lib()
+    for ys, B, H in (((0, 256, 64), 2, 1), ((256, 0, 64), 1, 2)):
+        assert L.tlin_rope(rope_params(B=B, H=H, y_stride=ys), A, 2 * A, A, A, None) == 1
+    assert L.tlin_rope(rope_params(B=1 << 20, rows=1 << 10, D=8, rot=8, H=1 << 10), A, 2 * A, A, A, None) == 2      # more than a launch takes
+    g = [None, None, A, A, A, A, A, A, A, None]
+    for kw in (dict(kp_stride=(0, 1024, 64)), dict(kp_stride=(2048, 0, 64)), dict(vp_stride=(0, 1024, 64)), dict(vp_stride=(2048, 0, 64))):
+        assert L.tlin_paged_append(packed_paged(**kw), None, *g, None) == 1
+    assert L.tlin_paged_append(packed_paged(o_stride=(0, 64)), rope_params(), A, 2 * A, *g[2:9], A, None) == 1
+    assert L.tlin_paged_attn(packed_paged(o_stride=(0, 64)), A, A, A, A, A, A, A, None, A, 1 << 40, None) == 1
+    cache_p = lambda *st: b.packed(b.TlinCacheParams, b.CACHE_LAYOUT, 1, 9, 2, 16, 64, 1, 0, 0, *st)  # noqa: E731
+    for a, c in (((0, 1024, 64), (0, 0, 0)), ((0, 0, 0), (2048, 0, 64))):
+        assert L.tlin_pages_copy(cache_p(*a, *c), A, A, A, None, 1, None) == 1
+
+
+def test_wrappers_refuse_rows_that_lie_on_one_another():
+    """Expanded tensors whose strides are all 0 would be taken for dense ones."""
+    from paper_2508_20407_amd import paged
+    x = torch.zeros(64)
+    for t in (x.expand(2, 3, 4, 64), x.expand(1, 1, 4, 64)):
+        with pytest.raises(ValueError, match="on one another"):
+            paged._rows(t, 4, "x")
+    assert paged._rows(x.expand(2, 3, 1, 64), 4, "x") == (0, 0, 64)
+    with pytest.raises(ValueError, match="on one another"):
+        paged._table_stride(ints([1, 2]).expand(3, 2), 3)
+    assert paged._table_stride(ints([1, 2]).expand(1, 2), 1) == 0
+    k = torch.zeros((2, 2, 16, 64))
+    one = k[:, :, :1].expand(2, 2, 16, 64)
+    for kp, vp in ((one, k), (k, one)):
+        with pytest.raises(ValueError):
+            paged._paged(-1, kp, vp, ints([[0]]), ints([1]), ints([0, 1]), 1, 2, 1, 0, 0, True, 1.0, (0,) * 8)
+
+
+@gpu
+def test_broadcast_inputs():
+    """What is read may repeat by a stride of 0: batches and heads of a rotation, new rows of all heads, one page for all."""
+    gen = torch.Generator().manual_seed(17)
+    x = torch.randn((1, 1, 5, 64), generator=gen).cuda()
+    pos, freqs = ints([0, 3, 5, 9, 1000]).cuda(), tl.rope_frequencies(64)[0]
+    want = tl.tlin_rope(x, pos, freqs)
+    for t in (x.expand(2, 1, 5, 64), x.expand(1, 3, 5, 64), x.expand(2, 3, 5, 64), x[:, :, :1].expand(2, 3, 1, 64)):
+        got = tl.tlin_rope(t, pos[:t.shape[2]], freqs, out=torch.empty(t.shape, device="cuda"))
+        assert torch.equal(got, want[:, :, :t.shape[2]].expand(t.shape))
+    k, v, table = (t.cuda() for t in cache(gen, torch.float32, [40, 33], 2, 64, 16))
+    lens, starts = ints([40, 33]).cuda(), ints([0, 3, 5]).cuda()
+    for s in (1, 0):
+        kp, vp = k.clone(), v.clone()
+        row = x[0, :, :5].expand(2, 5, 64) if s else x[0].expand(2, 5, 64).contiguous()
+        tl.tlin_paged_append(row, row, kp, vp, table, lens, starts, q=row, q_out=torch.empty((2, 5, 64), device="cuda"), freqs=freqs)
+        o = tl.tlin_paged_attn(row, kp, vp, table, lens, starts, max_rows=3, out=torch.empty((2, 5, 64), device="cuda"))
+        if s:
+            first = (kp, vp, o)
+    for a, c in zip(first, (kp, vp, o)):
+        assert torch.equal(torch.nan_to_num(a), torch.nan_to_num(c))
+
+
 def test_structures_match_the_header():
     for cls, layout, size in ((b.TlinRopeParams, b.ROPE_LAYOUT, 88), (b.TlinPagedParams, b.PAGED_LAYOUT, 168),
                               (b.TlinBookParams, b.BOOK_LAYOUT, 20), (b.TlinCacheParams, b.CACHE_LAYOUT, 88)):
