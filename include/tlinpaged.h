@@ -113,8 +113,7 @@ typedef struct {
 } tlin_book_params;
 
 /* Every listed sequence gives up its pages: refs of each one less, its table row -1, its length 0.  seqs int32 [n], n
- * at most 65536.  A
- * sequence listed twice is freed once; ids outside [0, S) are passed over. */
+ * at most 65536.  A sequence listed twice is freed once; ids outside [0, S) are passed over. */
 tlin_status tlin_pages_free(const tlin_book_params *p, int32_t *table, int32_t *lens, int32_t *refs, const int32_t *seqs,
                             int32_t n, void *stream);
 
