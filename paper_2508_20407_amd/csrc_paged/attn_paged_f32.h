@@ -7,7 +7,10 @@
 // are fp32 throughout, and weights are 2^((s - m) c), so that the largest one is exactly 1.
 //
 // Bound by the matrix pipe (157 TFLOP/s): 64 instructions of 64 cycles each for the scores and the values of a tile at 128
-// columns, whatever the number of rows in the wave.
+// columns, whatever the number of rows in the wave.  Four columns behind whole blocks of 32 (36, 68, 100: TAIL) are summed by
+// vector instructions, 64 of 4 cycles in the place of a block's 16 of 64: a lane multiplies its sixteen weights with the four
+// values of each key, which all lanes of its half read at one address (3 windows of up to 250 rows over 9000, 12 heads x 36:
+// 131 -> 102 us; 512 over 4096, 32 heads x 100: 316 -> 271).
 //
 // Tiles go to LDS by direct loads, in groups of 16 rows that may lie in different pages, as in attn_paged_bf16.h.  K rows are
 // swizzled by row & 15 (16 lanes read 16 bytes of 16 rows at once), V rows by bit 2 of the row (the two halves of a wave
@@ -30,14 +33,14 @@ struct PagedF32 {
     static_assert(NDMA >= 1 && DU % 32 == 0, "tile does not divide over the waves");
 };
 
-template <int DU, int NW>
+template <int DU, int NW, bool TAIL>
 __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, bool direct, int64_t slot)
 {
     ConstPagedArgs &a = *args_again();
     using C = PagedF32<DU, NW>;
     constexpr int DK = C::DK, BN = C::BN, BM = C::BM, ROWB = C::ROWB, TILE_B = C::TILE_B, CPR = C::CPR, RPI = C::RPI;
     constexpr int NDMA = C::NDMA, NGW = C::NGW;
-    constexpr int DQ = DU / 8, DB = DU / 32;       // 16-byte reads of a key per lane, blocks of 32 output columns
+    constexpr int DQ = DU / 8, DB = DU / 32 - TAIL;       // 16-byte reads of a key per lane, blocks of 32 output columns
 
     char *const Ks = tlin_smem;
     char *const Vs = tlin_smem + 2 * TILE_B;
@@ -126,7 +129,10 @@ __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, b
 #pragma unroll
     for (int db = 0; db < DB; ++db) vaddr[db] = lds_offset(Vs) + 4 * h * ROWB + (((8 * db + (j >> 2)) ^ (h << 3)) << 4) + 4 * (j & 3);
 
+    const unsigned taddr = lds_offset(Vs) + 4 * h * ROWB + ((8 * DB ^ (h << 3)) << 4);      // the last four columns of the same keys
+
     f32x16 oacc[DB];
+    f32x4 tail = {0.f, 0.f, 0.f, 0.f};      // their sums over this half's keys
     float m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -180,6 +186,7 @@ __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, b
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) oacc[db][v] *= alpha;
+            if (TAIL) tail *= alpha;
             m = mn;
         }
         const float ref = m == -INFINITY ? 0.f : m;
@@ -191,41 +198,50 @@ __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, b
         }
         l += ls;
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
+        for (int v = 0; v < 16; ++v) {
+            if (TAIL) {
+                const f32x4 vt = *(lds_f32x4 *)(uintptr_t)(taddr + st + (8 * (v >> 2) + (v & 3)) * ROWB);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) tail[e] = fmaf(S[v], vt[e], tail[e]);
+            }
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
                 const float vf = *(lds_f32 *)(uintptr_t)(vaddr[db] + st + (8 * (v >> 2) + (v & 3)) * ROWB);
                 oacc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, S[v], oacc[db], 0, 0, 0);
             }
+        }
     }
 
     const float lt = xhalf_sum(l);
+    if (TAIL)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tail[e] = xhalf_sum(tail[e]);
     ConstPagedArgs &z = *args_again();
     if (mine) {
         const float inv = !direct ? 1.f : lt > 0.f ? 1.0f / lt : lt == 0.f ? 0.f : lt;
         const int64_t off = hd * z.o_sh + qrow * z.o_sr;
         float *op = z.Opart + (slot * BM + r) * DK;
+        auto put = [&](int d, f32x4 o) __attribute__((always_inline)) {
+            o *= inv;
+            if (!direct) {
+                *(f32x4 *)(op + d) = o;
+            } else if (d < z.D) {
+                if (z.out_bf16) {
+                    bf16x4 ob;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) ob[e] = (__bf16)o[e];
+                    *(bf16x4 *)((__bf16 *)z.O + off + d) = ob;
+                } else {
+                    *(f32x4 *)((float *)z.O + off + d) = o;
+                }
+            }
+        };
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int d = 32 * db + 8 * g + 4 * h;
-                f32x4 o;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = oacc[db][4 * g + e] * inv;
-                if (!direct) {
-                    *(f32x4 *)(op + d) = o;
-                } else if (d < z.D) {
-                    if (z.out_bf16) {
-                        bf16x4 ob;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) ob[e] = (__bf16)o[e];
-                        *(bf16x4 *)((__bf16 *)z.O + off + d) = ob;
-                    } else {
-                        *(f32x4 *)((float *)z.O + off + d) = o;
-                    }
-                }
-            }
+            for (int g = 0; g < 4; ++g)
+                put(32 * db + 8 * g + 4 * h, f32x4{oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2], oacc[db][4 * g + 3]});
+        if (TAIL && h == 0) put(32 * DB, tail);
         if (h == 0) {
             if (!direct) {
                 z.Mpart[slot * BM + r] = m * z.c;
@@ -239,14 +255,14 @@ __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, b
     __builtin_amdgcn_s_barrier();
 }
 
-template <int DU, int NW>
+template <int DU, int NW, bool TAIL>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 8)))
 void paged_f32_kernel(const PagedArgs)
 {
     using C = PagedF32<DU, NW>;
     __shared__ PlaceLds lds;
     share_items<C::BN>(xcd_remap(blockIdx.x, gridDim.x), lds, [](const Place &p, int t0, int t1, bool whole, int64_t slot) __attribute__((always_inline)) {
-        paged_f32_item<DU, NW>(p, t0, t1, whole, slot);
+        paged_f32_item<DU, NW, TAIL>(p, t0, t1, whole, slot);
     });
 }
 

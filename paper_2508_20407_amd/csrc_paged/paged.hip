@@ -152,10 +152,10 @@ tlin_status launch_paged_bf16(const PagedArgs &a, hipStream_t st)
     tlin_status s = allow_lds(kernel, lds, allowed);
     return s ? s : launch_kernel(kernel, dim3(a.shares), dim3(NW * 64), lds, st, a);
 }
-template <int DU, int NW>
+template <int DU, int NW, bool TAIL = false>
 tlin_status launch_paged_f32(const PagedArgs &a, hipStream_t st)
 {
-    const void *kernel = (const void *)paged_f32_kernel<DU, NW>;
+    const void *kernel = (const void *)paged_f32_kernel<DU, NW, TAIL>;
     constexpr int lds = PagedF32<DU, NW>::LDS_BYTES;
     static std::atomic<uint64_t> allowed{0};
     tlin_status s = allow_lds(kernel, lds, allowed);
@@ -169,6 +169,8 @@ tlin_status launch_paged_few(const PagedArgs &a, hipStream_t st)
 template <int DU>
 tlin_status launch_paged(const PagedArgs &a, const PagedShape &s, bool bf, bool nt, hipStream_t st)
 {
+    if constexpr (DU > 32)
+        if (!bf && a.D % 32 == 4) return s.nw == 2 ? launch_paged_f32<DU, 2, true>(a, st) : launch_paged_f32<DU, 4, true>(a, st);
     if (!bf) return s.nw == 2 ? launch_paged_f32<DU, 2>(a, st) : launch_paged_f32<DU, 4>(a, st);
     if (s.nw == 2) return nt ? launch_paged_bf16<DU, 2, true>(a, st) : launch_paged_bf16<DU, 2, false>(a, st);
     if (s.nw == 4) return launch_paged_bf16<DU, 4, false>(a, st);

@@ -141,6 +141,21 @@ def test_attention_head_dimensions(dtype, D):
 
 
 @gpu
+@pytest.mark.parametrize("D", [36, 68, 100, 40, 124])
+@pytest.mark.parametrize("most", [9, 20, 60])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_columns_behind_whole_blocks(D, most, causal):
+    """Heads of 32 n + 4 columns and beside them, in workgroups of two and of four waves, items cut and whole, missing pages."""
+    def edit(k, v, table, lens):
+        table[0, 3] = -1
+        table[2, 0] = k.shape[0]
+        v[table[3, 0].item(), :, 1] *= 100.0
+
+    check_attn("f32", [700, 12, 40, 65], [most, 1, 7, 33 if most > 33 else 2], 6, 2, D, 16, causal=causal, edit=edit, seed=D + most)
+    check_attn("f32", [40, 3], [2, 3], 20, 2, D, 16, causal=causal, out_dtype="bf16", seed=D)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("R", [16, 32, 64, 256])
 @pytest.mark.parametrize("causal", [True, False])
