@@ -19,6 +19,8 @@
  *     [heads, T, D], and they are the LAST rows of the sequence, which has lens[s] rows with them: row
  *     starts[s] + i is at position lens[s] - (starts[s+1] - starts[s]) + i.
  *   - A stride of 0 repeats what is read; a tensor that is written has none on an axis longer than one (refused).
+ *   - A workspace belongs to a call from its first launch to the end of its last.  Calls that share one follow each other
+ *     on one stream, all launches of one before the first of the next: two host threads that call at once have two.
  *   - Key heads may be shared: query head h reads key head h / (H / HK); HK divides H.
  *   - What the device arrays hold cannot be refused by the host, so the kernels check it: lengths are cut to
  *     what the table can name (table_width * page_rows) and starts to [0, T]; a page id outside

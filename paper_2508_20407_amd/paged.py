@@ -7,6 +7,7 @@ the table, lengths, starts and counts int32 tensors on the same device.  Nothing
 from __future__ import annotations
 
 import ctypes
+import threading
 
 import torch
 
@@ -115,22 +116,30 @@ def _call(index, stream, name, *args):
 
 
 _ws_bytes = {}     # what the library answered, by the sizes that it goes by
-_scratch = {}      # (device, stream) -> (aligned address, bytes behind it, buffer)
+
+
+class _Scratch(threading.local):
+    def __init__(self):
+        self.of = {}     # (device, stream) -> (aligned address, bytes behind it, buffer)
+
+
+_scratch = _Scratch()
 
 
 def _workspace(device, index, stream, workspace, nbytes):
-    """Device scratch, (address, bytes, what keeps it): the caller's, or one kept per device and stream and grown on demand.
-    A call that is captured gets scratch of its own from the graph's memory: graphs captured on one stream may be
-    replayed on two, and what is kept here may be replaced by a larger one."""
+    """Device scratch, (address, bytes, what keeps it): the caller's, or one kept per host thread, device and stream and grown
+    on demand.  Not per stream alone: calls of two threads on one stream may enqueue their launches in turn, and a call's
+    launches hand their results to each other here.  A call that is captured gets scratch of its own from the graph's memory:
+    graphs captured on one stream may be replayed on two, and what is kept here may be replaced by a larger one."""
     if workspace is not None:
         return (*workspace.get(nbytes, device), None)
-    have = _scratch.get((index, stream))
+    have = _scratch.of.get((index, stream))
     capturing = torch._C._cuda_isCurrentStreamCapturing()
     if have is None or have[1] < nbytes or capturing:
         buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
         have = ((buf.data_ptr() + 255) // 256 * 256, nbytes, buf)
         if not capturing:
-            _scratch[(index, stream)] = have
+            _scratch.of[(index, stream)] = have
     return have
 
 
