@@ -10,6 +10,8 @@ cache (see ``paged.py``).
 """
 from __future__ import annotations
 
+import threading
+
 from . import binding
 from .binding import (TLIN_BF16, TLIN_COMBINE_JOINT, TLIN_COMBINE_SUM, TLIN_F32, TlinError, TlinParams)
 
@@ -67,7 +69,8 @@ def params_for(q, n_hist, out_dtype=None, scale=None, num_splits=0, combine=TLIN
 
 
 class Workspace:
-    """Caller-owned device scratch for split partials, grown on demand and reused."""
+    """Caller-owned device scratch for split partials, grown on demand and reused.  Calls that share one follow each other:
+    on one stream, from one host thread at a time."""
 
     def __init__(self):
         self.buf = None
@@ -85,18 +88,23 @@ class Workspace:
         return (self.buf.data_ptr() + 255) // 256 * 256, nbytes
 
 
-# Calls that share a workspace must be ordered on one stream, so the workspaces the wrappers
-# fall back to are kept per (device, stream).
-_default_ws = {}
+# Calls that share a workspace must be ordered on one stream, all launches of one before the first of the
+# next, so the workspaces the wrappers fall back to are kept per host thread and (device, stream).
+class _DefaultWorkspaces(threading.local):
+    def __init__(self):
+        self.of = {}
+
+
+_default_ws = _DefaultWorkspaces()
 
 
 def _workspace_for(t, workspace, stream):
     if workspace is not None:
         return workspace
     key = (t.device, stream)
-    ws = _default_ws.get(key)
+    ws = _default_ws.of.get(key)
     if ws is None:
-        ws = _default_ws[key] = Workspace()
+        ws = _default_ws.of[key] = Workspace()
     return ws
 
 
