@@ -210,5 +210,20 @@ def tlin_slide_layer_attn(q, k_hist, v_hist, k_win, v_win, chunk, *, combine=TLI
     return o
 
 
-from .paged import (rope_frequencies, tlin_paged_append, tlin_paged_attn, tlin_pages_compact, tlin_pages_copy,  # noqa: E402
-                    tlin_pages_fork, tlin_pages_free, tlin_pages_reserve, tlin_rope)
+# The faces of the paged cache, imported with the first use of one: what needs no torch (the binding, the build, the cost
+# model) is imported without it.
+_PAGED = frozenset(("tlin_rope", "rope_frequencies", "tlin_paged_append", "tlin_paged_attn", "tlin_pages_reserve", "tlin_pages_fork",
+                    "tlin_pages_free", "tlin_pages_compact", "tlin_pages_copy"))
+
+
+def __getattr__(name):
+    if name != "paged" and name not in _PAGED:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    import importlib
+    paged = importlib.import_module(".paged", __name__)
+    globals().update({n: getattr(paged, n) for n in _PAGED})
+    return paged if name == "paged" else getattr(paged, name)
+
+
+def __dir__():
+    return sorted({*globals(), *__all__, "paged"})
