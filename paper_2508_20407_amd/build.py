@@ -22,6 +22,7 @@ HIPCC_FLAGS = [
 
 
 def build(verbose: bool = False, extra=()) -> str:
+    """The library's path.  extra: flags for every compile and for the link."""
     inc = ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"), "-I", os.path.join(HERE, "csrc_paged")]
     with tempfile.TemporaryDirectory() as tmp:
         objs, jobs = [], []
@@ -32,7 +33,7 @@ def build(verbose: bool = False, extra=()) -> str:
                 print(" ".join(cmd), flush=True)
             jobs.append(subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True))
         results = [(job.communicate()[1], job.returncode) for job in jobs]      # both run on side by side
-        link = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB_PATH]
+        link = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-Wno-unused-command-line-argument", *objs, *extra, "-o", LIB_PATH]
         if all(rc == 0 for _, rc in results):
             if verbose:
                 print(" ".join(link), flush=True)
