@@ -51,15 +51,29 @@ def _ints(name, t, index, size):
     raise ValueError(f"{name}: {size} entries, one after another, expected")
 
 
+_whole = {}        # strides -> those of the axes before D where the library takes them for axes of any length, else False
+
+
 def _rows(t, axes, name):
+    """Strides of the axes before D."""
     st = t.stride()
-    if len(st) != axes or (st[-1] != 1 and t.shape[-1] != 1):
+    known = _whole.get(st)
+    if known and len(known) == axes - 1:
+        return known
+    shape = t.shape
+    if len(st) != axes or (st[-1] != 1 and shape[-1] != 1):
         raise ValueError(f"{name}: {axes} axes expected, the last one contiguous")
-    if not st[-2]:           # (strides of zeros alone would be taken for those of a dense tensor)
-        if t.shape[-2] > 1:
-            raise ValueError(f"{name}: rows that lie on one another")
-        return (*st[:-2], (t.shape[-1] + 7) // 8 * 8)
-    return st[:-1]
+    if not st[-2] and shape[-2] > 1:
+        raise ValueError(f"{name}: rows that lie on one another")
+    if known is None:
+        if len(_whole) >= 4096:
+            _whole.clear()
+        known = _whole[st] = st[-1] == 1 and 0 < st[-2] < 1 << 23 and not any(s % 8 for s in st[:-1]) and st[:-1]
+    if known or 1 not in shape:
+        return st[:-1]
+    # The stride of an axis of one entry addresses nothing and may be any number: 0 stands for it, and for a row's a row of
+    # whole 16-byte pieces (strides of zeros alone would be taken for those of a dense tensor).
+    return (*(s if n > 1 else 0 for s, n in zip(st[:-2], shape)), st[-2] if shape[-2] > 1 else (shape[-1] + 7) // 8 * 8)
 
 
 def _table_stride(table, S):
@@ -67,6 +81,10 @@ def _table_stride(table, S):
     if S > 1 and not st:
         raise ValueError("table: rows that lie on one another")
     return st
+
+
+def _table_like(t, table):
+    return t.shape == table.shape and (t.shape[0] == 1 or t.stride(0) == table.stride(0))
 
 
 def _like(t, dtype=None):
@@ -207,6 +225,8 @@ def _paged(index, k_pages, v_pages, table, lens, starts, T, H, max_rows, code, o
         _rows(k_pages, 4, "k_pages"), _rows(v_pages, 4, "v_pages")
         raise ValueError("k_pages and v_pages must have the same shape")
     P, HK, R, D = shape
+    if P == 1 or HK == 1:           # (strides that may be any number)
+        kp, vp = _rows(k_pages, 4, "k_pages"), _rows(v_pages, 4, "v_pages")
     if table.dtype is not _I32 or table.get_device() != index or len(entries) != 2 or (entries[1] > 1 and table.stride(1) != 1):
         _table(index, table)
     S, M = entries
@@ -351,7 +371,8 @@ def tlin_pages_compact(table, refs, *, table_out=None, refs_out=None, workspace=
     t = table if table_out is None else table_out
     r = refs if refs_out is None else refs_out
     P = refs.shape[0]
-    if _table(index, t) != table.shape or t.stride() != table.stride():
+    _table(index, t)
+    if not _table_like(t, table):
         raise ValueError("table_out must have the shape and strides of table")
     _ints("refs_out", r, index, P)
     n = P // 2

@@ -72,3 +72,85 @@ def test_calls_of_two_host_threads_on_one_stream(dtype):
     for i in range(2):
         for one in got[i]:
             assert all(torch.equal(a, c) for a, c in zip(one, want[i]))
+
+
+# ---------------------------------------------------------------- axes of one entry
+def odd_views(dtype, H, D, device="cpu"):
+    """Single rows, heads and batches whose axis has a stride that addresses nothing and is no multiple of 16 bytes."""
+    row = -(-D // 8) * 8
+    base = torch.randn((H, row), generator=torch.Generator().manual_seed(D)).to(dtype).to(device)
+    one_row = base[:, :D].unsqueeze(1)                      # [H, 1, D], row stride D
+    one_head = base[:, :D].unsqueeze(0).unsqueeze(0)        # [1, 1, H, D] read as B = 1, one head, H rows: head stride H D'
+    one_head = one_head.as_strided(one_head.shape, (3, D + 1, row, 1))
+    return one_row, one_head
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [36, 100, 64])
+def test_strides_of_axes_of_one_entry_do_not_count(dtype, D):
+    one_row, one_head = odd_views(dtype, 4, D)
+    row = -(-D // 8) * 8
+    assert paged._rows(one_row, 3, "q") == (row, row)
+    assert paged._rows(one_head, 4, "x") == (0, 0, row)
+    assert paged._rows(one_row.as_strided((4, 1, D), (row, 1 << 40, 1)), 3, "q") == (row, row)
+    # caches of one head, of one page
+    pages = torch.zeros((5, 16, row), dtype=dtype)[..., :D].unsqueeze(1)
+    assert paged._rows(pages.as_strided(pages.shape, (16 * row, 7, row, 1)), 4, "k_pages") == (16 * row, 0, row)
+    with pytest.raises(ValueError, match="on one another"):
+        paged._rows(one_row[:, :1].expand(4, 2, D).as_strided((4, 2, D), (row, 0, 1)), 3, "q")
+
+
+def test_caches_of_one_head_or_one_page_are_packed_without_their_strides():
+    ints = lambda x: torch.tensor(x, dtype=torch.int32)  # noqa: E731
+    for P, HK in ((1, 2), (3, 1)):
+        plain = torch.zeros((P, HK, 16, 40), dtype=torch.bfloat16)[..., :36]
+        st = plain.stride()
+        odd = plain.as_strided(plain.shape, (13 if P == 1 else st[0], 13 if HK == 1 else st[1], st[2], 1))
+        args = (ints([[0]]), ints([1]), ints([0, 1]), 1, HK, 1, 1, 1, True, 1.0, (0,) * 8)
+        p = [paged.PAGED_LAYOUT.unpack(paged._paged(-1, k, v, *args))[-6:] for k, v in ((odd, odd), (odd, plain), (plain, plain))]
+        assert p[2] == (*st[:3], *st[:3])
+        for x in p:
+            assert all(n % 8 == 0 for n in x) and all(x[i] == x[i + 3] == st[i] for i in range(3) if plain.shape[i] > 1)
+
+
+def test_a_book_of_one_sequence_is_compacted_into_any_row():
+    ints = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    assert paged._table_like(ints((1, 8))[:, :5], ints((1, 5)))
+    assert paged._table_like(ints((3, 8))[:, :5], ints((3, 8))[:, 3:])
+    assert not paged._table_like(ints((3, 8))[:, :5], ints((3, 5)))
+    assert not paged._table_like(ints((3, 5)), ints((1, 5)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [36, 64, 100])
+def test_calls_with_axes_of_one_entry(dtype, D):
+    """What a call gives for such a view it gives for a dense copy."""
+    R, row = 16, -(-D // 8) * 8
+    f = tl.rope_frequencies(D)[0]
+    one_row, one_head = odd_views(dtype, 4, D, "cuda")
+    gen = torch.Generator().manual_seed(3)
+
+    def copy(t):
+        return torch.empty((*t.shape[:-1], row), dtype=t.dtype, device=t.device)[..., :D].copy_(t)
+
+    pos = torch.tensor([7, 8, 9, 1000], dtype=torch.int32).cuda()
+    assert torch.equal(tl.tlin_rope(one_head, pos, f), tl.tlin_rope(copy(one_head), pos, f))
+    cache = torch.randn((5, 1, R, row), generator=gen).to(dtype).cuda()[..., :D]
+    odd = cache.as_strided(cache.shape, (R * row, 13, row, 1))
+    table, wide = torch.tensor([[4, 0, 2]], dtype=torch.int32).cuda(), torch.full((1, 9), -1, dtype=torch.int32).cuda()
+    lens, starts = torch.tensor([40], dtype=torch.int32).cuda(), torch.tensor([0, 1], dtype=torch.int32).cuda()
+    got = []
+    for q, c in ((one_row, odd), (copy(one_row), cache)):
+        kp, vp = (torch.zeros((5, 1, R, row), dtype=dtype, device="cuda")[..., :D] for _ in range(2))
+        kp.copy_(cache)
+        kp, vp = (t.as_strided(c.shape, c.stride()) for t in (kp, vp))
+        qr = tl.tlin_paged_append(q[:1], q[1:2], kp, vp, table, lens, starts, q=q, freqs=f)
+        o = tl.tlin_paged_attn(qr, kp, c, table, lens, starts, max_rows=1)
+        tl.tlin_pages_copy(kp, None, torch.tensor([[4, 1]], dtype=torch.int32).cuda())
+        got.append((qr, o, *(torch.stack([t[i, 0] for i in range(5)]) for t in (kp, vp))))
+    for a, c in zip(*got):
+        assert torch.equal(a, c)
+    refs = torch.tensor([1, 0, 1, 0, 1], dtype=torch.int32).cuda()
+    t, r, moves, count = tl.tlin_pages_compact(table, refs, table_out=wide[:, 3:6], refs_out=torch.empty_like(refs))
+    assert t.tolist() == [[1, 0, 2]] and wide[0, :3].tolist() == [-1] * 3 and count.item() == 1
