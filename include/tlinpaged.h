@@ -15,6 +15,7 @@
  * whole pieces), launches on `stream` without synchronising, nothing allocated, errors by return code, checks
  * on the host before any HIP call, capture into a HIP graph once a call of the same shape has run outside one.
  * What differs:
+ *   - Strides are below 2^47 bytes (refused).
  *   - New rows are ragged: those of sequence s are rows starts[s] .. starts[s+1]-1 of tensors
  *     [heads, T, D], and they are the LAST rows of the sequence, which has lens[s] rows with them: row
  *     starts[s] + i is at position lens[s] - (starts[s+1] - starts[s]) + i.

@@ -50,6 +50,7 @@ tlin_status allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &done
 }
 
 constexpr int kMaxRows = 1 << 30;
+constexpr int64_t kMaxBytes = (int64_t)1 << 47;      // of a stride: what device addresses reach (and products of it and a type's size fit)
 
 inline bool is_type(int32_t t) { return t == TLIN_F32 || t == TLIN_BF16; }
 inline int bytes_of(int32_t t) { return t == TLIN_F32 ? 4 : 2; }
@@ -59,7 +60,7 @@ inline bool good_page_rows(int32_t r) { return r >= 16 && r <= 65536 && (r & (r 
 inline int log2_of(int32_t r) { return __builtin_ctz((unsigned)r); }
 
 // Strides of a tensor of n axes before D: all 0 = dense (which needs rows of whole 16-byte pieces), else multiples
-// of 16 bytes, rows owning their pieces and (32-bit offsets inside a tile) below 32 MiB apart.
+// of 16 bytes and below kMaxBytes, rows owning their pieces and (32-bit offsets inside a tile) below 32 MiB apart.
 template <int N>
 tlin_status check_strides(const int64_t (&s)[N], int D, int eb)
 {
@@ -67,7 +68,7 @@ tlin_status check_strides(const int64_t (&s)[N], int D, int eb)
     for (int i = 0; i < N; ++i) zero = zero && s[i] == 0;
     if (zero) return D % (16 / eb) ? TLIN_ERR_INVALID_ARG : TLIN_OK;
     for (int i = 0; i < N; ++i)
-        if (s[i] < 0 || s[i] % (16 / eb)) return TLIN_ERR_INVALID_ARG;
+        if (s[i] < 0 || s[i] % (16 / eb) || s[i] >= kMaxBytes / eb) return TLIN_ERR_INVALID_ARG;
     if (s[N - 1] < row_elements(D, eb) || s[N - 1] * eb >= (int64_t)1 << 25) return TLIN_ERR_INVALID_ARG;
     return TLIN_OK;
 }

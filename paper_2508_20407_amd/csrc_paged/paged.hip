@@ -133,14 +133,17 @@ PagedShape paged_shape(const tlin_paged_params *p)
 }
 
 struct PagedWorkspace { float *O, *M, *L; CutItem *cuts; };
-size_t paged_workspace(const PagedShape &s, void *ws, PagedWorkspace &w)
+size_t workspace_rows(const PagedShape &s) { return 2 * (size_t)s.shares * s.bm(); }
+size_t workspace_bytes(const PagedShape &s) { return workspace_rows(s) * (s.dk + 2) * sizeof(float) + s.shares * sizeof(CutItem); }
+PagedWorkspace workspace_of(const PagedShape &s, void *ws)
 {
-    const size_t rows = 2 * (size_t)s.shares * s.bm();
+    const size_t rows = workspace_rows(s);
+    PagedWorkspace w;
     w.O = (float *)ws;
     w.M = w.O + rows * s.dk;
     w.L = w.M + rows;
     w.cuts = (CutItem *)(w.L + rows);
-    return (rows * s.dk + 2 * rows) * sizeof(float) + s.shares * sizeof(CutItem);
+    return w;
 }
 
 template <int DU, int NW, bool NT>
@@ -180,7 +183,7 @@ tlin_status launch_paged(const PagedArgs &a, const PagedShape &s, bool bf, bool 
 
 // Threads to a row's partials: eight where there are too few rows to fill the chip with one.
 template <int DK>
-tlin_status launch_paged_merge(const PagedArgs &a, int64_t items, hipStream_t st)
+tlin_status launch_paged_merge(const PagedArgs &a, double items, hipStream_t st)
 {
     const int rows = a.TB * a.G;
     const bool many = items * rows * (DK / 4) < kNumCU * 512;
@@ -310,9 +313,7 @@ tlin_status tlin_paged_append(const tlin_paged_params *p, const tlin_rope_params
 
 size_t tlin_paged_workspace_bytes(const tlin_paged_params *p)
 {
-    if (check_paged(p)) return 0;
-    PagedWorkspace w;
-    return paged_workspace(paged_shape(p), nullptr, w);
+    return check_paged(p) ? 0 : workspace_bytes(paged_shape(p));
 }
 
 tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const void *k_pages, const void *v_pages,
@@ -336,8 +337,7 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
     const PagedShape s = paged_shape(p);
     const bool bf = p->dtype == TLIN_BF16;
     PagedArgs a = {};
-    PagedWorkspace w;
-    paged_workspace(s, ws, w);
+    const PagedWorkspace w = workspace_of(s, ws);
     a.Q = q; a.K = k_pages; a.V = v_pages;
     a.table = table; a.lens = lens; a.starts = starts;
     a.O = O; a.lse = lse;
@@ -376,13 +376,13 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
     // Rows that are read once by a call and exceed the last-level cache (256 MB) carry the non-temporal hint, by what the
     // table and the cache can hold of them.
     const int64_t named = (int64_t)p->S * p->table_width, most = named < p->num_pages ? named : p->num_pages;
-    const bool nt = p->max_rows <= s.tb && most * p->HK * p->page_rows * p->D * 4 >= (int64_t)192 << 20;
+    const bool nt = p->max_rows <= s.tb && (double)most * p->HK * p->page_rows * p->D * 4 >= 192 << 20;
     const int du = (p->D + 31) / 32 * 32;
     st = s.few ? (s.dk == 64 ? launch_paged_few<64>(a, hs) : launch_paged_few<128>(a, hs))
          : du == 32 ? launch_paged<32>(a, s, bf, nt, hs) : du == 64 ? launch_paged<64>(a, s, bf, nt, hs)
          : du == 96 ? launch_paged<96>(a, s, bf, nt, hs) : launch_paged<128>(a, s, bf, nt, hs);
     if (st) return st;
-    const int64_t items = (int64_t)p->S * p->HK * ((p->max_rows + s.tb - 1) / s.tb);
+    const double items = (double)p->S * p->HK * ((p->max_rows + s.tb - 1) / s.tb);
     return s.dk == 64 ? launch_paged_merge<64>(a, items, hs) : launch_paged_merge<128>(a, items, hs);
 }
 
@@ -480,7 +480,8 @@ tlin_status tlin_pages_copy(const tlin_cache_params *p, void *a, void *b, const 
     resolve(p->a_stride, sizes, p->D, strides[0]);
     resolve(p->b_stride, sizes, p->D, strides[1]);
     for (int c = 0; c < (b ? 2 : 1); ++c) {
-        if (p->layer_stride[c] < 0 || p->layer_stride[c] % (16 / eb)) return TLIN_ERR_INVALID_ARG;
+        if (p->layer_stride[c] < 0 || p->layer_stride[c] % (16 / eb) || p->layer_stride[c] >= kMaxBytes / eb) return TLIN_ERR_INVALID_ARG;
+        if (p->layers > 1 && !p->layer_stride[c] && strides[c][0] >= kMaxBytes / eb / p->num_pages) return TLIN_ERR_INVALID_ARG;
         if (written_twice(strides[c], outer)) return TLIN_ERR_INVALID_ARG;
     }
     if (max_moves == 0) return TLIN_OK;
@@ -495,7 +496,7 @@ tlin_status tlin_pages_copy(const tlin_cache_params *p, void *a, void *b, const 
     for (int c = 0; c < g.caches; ++c) {
         const int64_t(&s)[3] = strides[c];
         g.cache[c] = (char *)(c == 0 ? a : b);
-        g.layer[c] = (p->layer_stride[c] ? p->layer_stride[c] : s[0] * p->num_pages) * eb;
+        g.layer[c] = p->layers == 1 ? 0 : (p->layer_stride[c] ? p->layer_stride[c] : s[0] * p->num_pages) * eb;
         g.page[c] = s[0] * eb; g.head[c] = s[1] * eb; g.row[c] = s[2] * eb;
         // heads outside rows or rows outside heads, without gaps
         g.flat[c] = (s[2] == re && s[1] == (int64_t)re * p->page_rows) || (s[1] == re && s[2] == (int64_t)re * p->HK) || (p->HK == 1 && s[2] == re);
