@@ -81,7 +81,7 @@ typedef struct {
     int32_t dtype;        /* tlin_dtype of queries, cache and new rows */
     int32_t out_dtype;    /* tlin_dtype of O (tlin_paged_attn) */
     int32_t causal;       /* new row i of a sequence sees the rows up to its own position; 0: all lens[s] rows */
-    float scale;          /* logit multiplier, finite and > 0 */
+    float scale;          /* logit multiplier, > 0, its product with log2(e) finite (as logits have to be in fp32) */
     int32_t table_stride; /* elements from one sequence's table row to the next; 0 = table_width */
     /* {head, row} of [heads, T, D] tensors, {page, head, row} of the caches [num_pages, HK, page_rows, D]; all 0 =
      * dense.  Row strides below 32 MiB; a cache's page stride, and page_rows row strides, below 4 GiB. */

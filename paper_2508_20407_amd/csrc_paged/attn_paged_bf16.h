@@ -186,7 +186,7 @@ __device__ __forceinline__ void paged_bf16_item(const Place &p, int t0, int t1, 
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int v = 0; v < 16; ++v) oacc[db][v] = 0.f;
-    const float thr = 8.0f / a.c;
+    const float thr = reference_step(a.c);
     bf16x8 pb[2][2];
     typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 

@@ -138,7 +138,7 @@ __device__ __forceinline__ void paged_f32_item(const Place &p, int t0, int t1, b
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int v = 0; v < 16; ++v) oacc[db][v] = 0.f;
-    const float thr = 8.0f / a.c;
+    const float thr = reference_step(a.c);
     const int D = a.D;
 
     asm volatile("" : "+v"(idA), "+v"(idB));

@@ -103,7 +103,7 @@ __device__ __forceinline__ void paged_f32_few_item(const Place &p, int t0, int t
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int e = 0; e < 4; ++e) O[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const float c = a.c, thr = 8.0f / c;
+    const float c = a.c, thr = reference_step(c);
     auto compute = [&](const Tile &x, int n, bool gone) __attribute__((always_inline)) {
         const int key = (t0 + n) * BN;
         f32x4 S = {0.f, 0.f, 0.f, 0.f};

@@ -322,7 +322,8 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
 {
     tlin_status st = check_paged(p);
     if (st) return st;
-    if (!(p->scale > 0.f) || !isfinite(p->scale)) return TLIN_ERR_INVALID_ARG;
+    const float c = p->scale * 1.4426950408889634f;
+    if (!(p->scale > 0.f) || !isfinite(c)) return TLIN_ERR_INVALID_ARG;
     if ((st = check_strides(p->q_stride, p->D, bytes_of(p->dtype))) || (st = check_strides(p->o_stride, p->D, bytes_of(p->out_dtype)))) return st;
     if (!q || !k_pages || !v_pages || !table || !lens || !starts || !O) return TLIN_ERR_INVALID_ARG;
     if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(O, 16)) return TLIN_ERR_INVALID_ARG;
@@ -370,7 +371,7 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
     a.causal = p->causal != 0;
     a.out_bf16 = p->out_dtype == TLIN_BF16;
     a.scale = p->scale;
-    a.c = p->scale * 1.4426950408889634f;
+    a.c = c;
 
     const hipStream_t hs = (hipStream_t)stream;
     // Rows that are read once by a call and exceed the last-level cache (256 MB) carry the non-temporal hint, by what the

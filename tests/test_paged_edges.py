@@ -5,7 +5,9 @@ import pytest
 import torch
 
 import paper_2508_20407_amd as tl
+from paper_2508_20407_amd import binding as b
 from paper_2508_20407_amd import paged
+from test_paged import A, check_attn, packed_paged
 
 
 def in_two_threads(f):
@@ -154,3 +156,21 @@ def test_calls_with_axes_of_one_entry(dtype, D):
     refs = torch.tensor([1, 0, 1, 0, 1], dtype=torch.int32).cuda()
     t, r, moves, count = tl.tlin_pages_compact(table, refs, table_out=wide[:, 3:6], refs_out=torch.empty_like(refs))
     assert t.tolist() == [[1, 0, 2]] and wide[0, :3].tolist() == [-1] * 3 and count.item() == 1
+
+
+# ---------------------------------------------------------------- scales
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [1e-45, 1e-39, 1.2e-38, 1e-37, 1e-20])
+def test_attention_of_the_smallest_scales(dtype, scale):
+    """Weights all but alike, whole items and cut ones, few rows and many."""
+    check_attn(dtype, [70, 9001, 33], [5, 1, 33], 6, 3, 64, 16, scale=scale)
+    check_attn(dtype, [40, 9001], [1, 2], 4, 2, 100, 16, scale=scale)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the accepted call would run on fake addresses")
+def test_scales_whose_base_2_form_is_not_finite_are_refused():
+    """Logits are taken in base-2 units: scale log2(e) has to be a number."""
+    call = lambda s: b.lib().tlin_paged_attn(packed_paged(scale=s), A, A, A, A, A, A, A, None, A, 1 << 40, None)  # noqa: E731
+    assert call(3e38) == call(2.4e38) == b.TLIN_ERR_INVALID_ARG
+    assert call(2.3e38) == b.TLIN_ERR_HIP            # every check is passed: the first thing that fails is the missing device
