@@ -152,7 +152,11 @@ def _workspace(device, index, stream, workspace, nbytes):
     if workspace is not None:
         return (*workspace.get(nbytes, device), None)
     have = _scratch.of.get((index, stream))
-    capturing = torch._C._cuda_isCurrentStreamCapturing()
+    if torch._C._cuda_getDevice() == index:
+        capturing = torch._C._cuda_isCurrentStreamCapturing()
+    else:
+        with torch.cuda.device(index):
+            capturing = torch._C._cuda_isCurrentStreamCapturing()
     if have is None or have[1] < nbytes or capturing:
         buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
         have = ((buf.data_ptr() + 255) // 256 * 256, nbytes, buf)

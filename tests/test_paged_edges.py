@@ -174,3 +174,32 @@ def test_scales_whose_base_2_form_is_not_finite_are_refused():
     call = lambda s: b.lib().tlin_paged_attn(packed_paged(scale=s), A, A, A, A, A, A, A, None, A, 1 << 40, None)  # noqa: E731
     assert call(3e38) == call(2.4e38) == b.TLIN_ERR_INVALID_ARG
     assert call(2.3e38) == b.TLIN_ERR_HIP            # every check is passed: the first thing that fails is the missing device
+
+
+# ---------------------------------------------------------------- devices
+def test_a_capture_on_the_tensors_device_is_seen_from_another(monkeypatch):
+    """Whether a call is captured is asked of the device whose stream it goes to, whichever device is current: scratch of a
+    captured call is the graph's and is not kept for later calls."""
+    current, streams_captured = [0], {1}
+
+    class on:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.index
+
+        def __exit__(self, *_):
+            current[0] = self.before
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0])
+    monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: current[0] in streams_captured)
+    monkeypatch.setattr(torch.cuda, "device", on)
+    monkeypatch.setattr(paged, "_scratch", paged._Scratch())
+    device = torch.device("cpu")
+    taken = paged._workspace(device, 1, 5, None, 500)
+    assert not paged._scratch.of                       # device 0 is current, the call's stream on device 1 is captured
+    with on(1):
+        kept = paged._workspace(device, 0, 5, None, 500)
+    assert paged._scratch.of == {(0, 5): kept}         # and the other way round: what is captured is not this call
+    assert taken[0] != kept[0] and current == [0]
