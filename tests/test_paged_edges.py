@@ -1,4 +1,9 @@
 """The paged cache where calls meet: host threads, devices, captures, shapes of one, the ends of the number ranges."""
+import ctypes
+import os
+import re
+import shutil
+import subprocess
 import threading
 
 import pytest
@@ -7,7 +12,9 @@ import torch
 import paper_2508_20407_amd as tl
 from paper_2508_20407_amd import binding as b
 from paper_2508_20407_amd import paged
-from test_paged import A, check_attn, packed_paged
+from test_paged import A, HB, U, attend, cache, check_attn, cuda, ints, packed_paged
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def in_two_threads(f):
@@ -203,3 +210,71 @@ def test_a_capture_on_the_tensors_device_is_seen_from_another(monkeypatch):
         kept = paged._workspace(device, 0, 5, None, 500)
     assert paged._scratch.of == {(0, 5): kept}         # and the other way round: what is captured is not this call
     assert taken[0] != kept[0] and current == [0]
+
+
+# ---------------------------------------------------------------- starts
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("starts,clean", [
+    ([-9, 2, 2, 1 << 30], [0, 2, 2, 8]),                  # cut to the rows there are
+    ([-(1 << 31), 1, 4, (1 << 31) - 1], [0, 1, 4, 8]),
+    ([2, 4, 0, 2], [2, 4, 0, 2]),                         # falling: none between, rows 4 to 7 are nobody's
+    ([5, 8, 3, 5], [5, 8, 3, 5]), ([8, 9, 12, 5], [8, 8, 8, 5])])
+@pytest.mark.parametrize("max_rows", [1, 8])
+def test_attention_with_starts_that_are_cut_or_fall(dtype, starts, clean, max_rows):
+    """Sound sequences come out right, and nothing but their rows is written."""
+    gen = torch.Generator().manual_seed(6)
+    lens, H, T, D, R = [64, 50, 40], 4, 8, 64, 16
+    k, v, table = cache(gen, dtype, lens, 2, D, R)
+    wide = torch.randn((H, 3 * T, D), generator=gen).to(dtype)
+    q = wide[:, T:2 * T]
+    out = torch.full_like(wide, 7.0).cuda()
+    tl.tlin_paged_attn(cuda(q), cuda(k), cuda(v), table.cuda(), ints(lens).cuda(), ints(starts).cuda(), max_rows=max_rows,
+                       out=out[:, T:2 * T])
+    want, _, bound, _ = attend(q, k, v, table, lens, clean, True, D ** -0.5, k.shape[0])
+    own = ~torch.isnan(want[0, :, 0])
+    assert own.sum().item() == sum(max(e - a, 0) for a, e in zip(clean, clean[1:]))
+    got = out[:, T:2 * T].cpu().double()
+    bound = bound + (HB * 1.01 if dtype == torch.bfloat16 else 2 * U) * want.abs()
+    assert ((got - want).abs()[:, own] <= bound[:, own]).all()
+    assert (got[:, ~own] == 7.0).all() and (out[:, :T] == 7.0).all() and (out[:, 2 * T:] == 7.0).all()
+
+
+# ---------------------------------------------------------------- sources
+@pytest.mark.skipif(shutil.which("gcc") is None, reason="gcc not found")
+def test_structures_have_the_offsets_that_the_headers_give_them(tmp_path):
+    pairs = {"tlin_params": b.TlinParams, "tlin_rope_params": b.TlinRopeParams, "tlin_paged_params": b.TlinPagedParams,
+             "tlin_book_params": b.TlinBookParams, "tlin_cache_params": b.TlinCacheParams}
+    lines = []
+    for name, cls in pairs.items():
+        lines.append(f'printf("%zu\\n", sizeof({name}));')
+        lines += [f'printf("%zu %zu\\n", offsetof({name}, {f[0]}), sizeof((({name} *)0)->{f[0]}));' for f in cls._fields_]
+    source, exe = tmp_path / "layout.c", tmp_path / "layout"
+    source.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "tlinpaged.h"\nint main(void)\n{\n' + "\n".join(lines) + "\nreturn 0;\n}\n")
+    subprocess.run(["gcc", "-I", os.path.join(ROOT, "include"), str(source), "-o", str(exe)], check=True)
+    said = iter(subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.splitlines())
+    for name, cls in pairs.items():
+        assert int(next(said)) == ctypes.sizeof(cls), name
+        for f in cls._fields_:
+            at = getattr(cls, f[0])
+            assert next(said) == f"{at.offset} {at.size}", (name, f[0])
+    for cls, layout in ((b.TlinRopeParams, b.ROPE_LAYOUT), (b.TlinPagedParams, b.PAGED_LAYOUT), (b.TlinBookParams, b.BOOK_LAYOUT),
+                        (b.TlinCacheParams, b.CACHE_LAYOUT)):
+        n = [1 if not hasattr(f[1], "_length_") else f[1]._length_ for f in cls._fields_]
+        p = b.packed(cls, layout, *range(1, sum(n) + 1))
+        got = [x for f, m in zip(cls._fields_, n) for x in ([getattr(p, f[0])] if m == 1 else list(getattr(p, f[0])))]
+        assert got == list(range(1, sum(n) + 1)), cls
+
+
+def test_inline_assembly_of_the_paged_cache_holds_no_instructions():
+    """The compiler takes the output of an assembly load as there at once: the paged kernels' direct loads and waits are those of
+    csrc/, their own assembly only orders what the compiler does."""
+    csrc = os.path.join(ROOT, "paper_2508_20407_amd", "csrc_paged")
+    texts = []
+    for name in sorted(os.listdir(csrc)):
+        source = open(os.path.join(csrc, name)).read()
+        texts += [(name, t) for t in re.findall(r"\basm\b(?:\s+volatile)?\s*\(\s*((?:\"[^\"]*\"\s*)*)", source)]
+        assert len(re.findall(r"\basm\b", source)) == len([t for n, t in texts if n == name]), name
+    assert texts
+    ops = sorted({(n, t.strip()) for n, t in texts if t.strip() != '""'})
+    assert ops == [("attn_paged_bf16.h", '"s_waitcnt lgkmcnt(0)"')]
