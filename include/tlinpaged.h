@@ -77,7 +77,8 @@ typedef struct {
     int32_t table_width;  /* pages that a row of the table can name */
     int32_t num_pages;    /* pages of the cache; table_width * page_rows at most 2^30 */
     int32_t max_rows;     /* most new rows of one sequence as far as the caller knows, in [1, T]: picks the kernel's
-                             shape; results do not depend on it */
+                             shape; results do not depend on it, times do: T for a step of single rows fills
+                             workgroups of up to 256 rows with a few */
     int32_t dtype;        /* tlin_dtype of queries, cache and new rows */
     int32_t out_dtype;    /* tlin_dtype of O (tlin_paged_attn) */
     int32_t causal;       /* new row i of a sequence sees the rows up to its own position; 0: all lens[s] rows */
@@ -91,7 +92,8 @@ typedef struct {
 /* Puts the new rows k, v [HK, T, D] into the pages at their positions.  With r (rot, interleaved, amplitude of it
  * are used) and freqs, keys are rotated on the way, and so are the queries q [H, T, D] into q_out [H, T, D] (both
  * NULL: no queries; q_out may be q).  r NULL: nothing is rotated, q is not taken.  Strides: q_stride, o_stride
- * (q_out), k_stride, v_stride.  Reserve the pages first; a page must belong to one sequence alone. */
+ * (q_out), k_stride, v_stride.  Reserve the pages first; a page must belong to one sequence alone.  More rows than a
+ * launch has workgroups for are TLIN_ERR_UNSUPPORTED, as in tlin_rope. */
 tlin_status tlin_paged_append(const tlin_paged_params *p, const tlin_rope_params *r, const void *q, void *q_out,
                               const void *k, const void *v, void *k_pages, void *v_pages, const int32_t *table,
                               const int32_t *lens, const int32_t *starts, const double *freqs, void *stream);
@@ -101,6 +103,7 @@ tlin_status tlin_paged_append(const tlin_paged_params *p, const tlin_rope_params
  * A row that sees nothing gets zeros and -infinity.  Rows of O that belong to no sequence are left as they were.
  * ws: tlin_paged_workspace_bytes(p) bytes, 256-byte aligned.  The work is cut into equal shares of rows seen, whatever
  * the lengths are, on the device; results do not depend on the order in which shares run.
+ * bf16: logits, weights and their sums are fp32, the weights rounded to bf16 for the value product, whatever out_dtype is.
  * Values of rows that a new row does not see, but another row of the call does, must be finite. */
 size_t tlin_paged_workspace_bytes(const tlin_paged_params *p);
 tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const void *k_pages, const void *v_pages,

@@ -5,7 +5,9 @@
 // arithmetic of tile n runs under the score products of tile n + 1 and the value products of tile n; K and V tiles of 64
 // rows by direct loads into a ring of two stages, swizzled on the source side; the reference point of a row moves only
 // where a logit exceeds it by 8 base-2 units; row sums in fp32 from the fp32 weights, which are rounded to bf16 for the
-// value product alone (relative error 2^-9 a weight, that averages out over a row's keys).
+// value product alone, whose operands are of one type: a weight is off by 2^-8 of itself at most, by
+// 1.66e-3 in the root mean square, and so is a sum over values of either sign (2.1 to 2.4e-3 with a bf16 result's own rounding, which
+// alone is 1.7e-3).
 //
 // What paging changes:
 //   - Rows come from pages of 16 or more rows, so a tile is four groups of 16 rows that lie anywhere.  A direct load covers 4

@@ -4,7 +4,8 @@
 // one query column a lane, which is the B operand of O^T[d, query] += V^T P^T as it stands: step v of the value product
 // contracts keys 8 (v / 4) + v % 4 (lanes 0 to 31) and the same + 4 (lanes 32 to 63), the ones that register v holds.
 // The contraction over columns is taken in the order in which 16-byte reads deliver them.  Products, weights and sums
-// are fp32 throughout, and weights are 2^((s - m) c), so that the largest one is exactly 1.
+// are fp32 throughout.  Weights are 2^((s - m) c), m the reference point of the row, which moves only where a logit exceeds it
+// by 8 base-2 units (any point gives the same result): they reach 256.
 //
 // Bound by the matrix pipe (157 TFLOP/s): 64 instructions of 64 cycles each for the scores and the values of a tile at 128
 // columns, whatever the number of rows in the wave.  Four columns behind whole blocks of 32 (36, 68, 100: TAIL) are summed by

@@ -11,7 +11,6 @@ namespace tlin {
 
 constexpr int kMergeThreads = 256;
 
-// LN threads share a (row, 4 columns): each takes every LN-th partial.  ROWS rows of the block at blockIdx.y.
 // LN threads share a (row, 4 columns): each takes every LN-th partial.  blockIdx.y: which of the item's rows.
 template <int DK, int LN>
 __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(const PagedArgs a)

@@ -361,12 +361,13 @@ tlin_status tlin_paged_attn(const tlin_paged_params *p, const void *q, const voi
     a.shares = s.shares;
     a.per_share = 1.0 / s.shares;
     a.per_G = 1.0f / a.G;
-    // What starting an item costs (page ids, queries, first tiles, output: 4 to 8 us), in rows of the cache, by which
-    // the times of uneven batches came out lowest.  bf16: 64 sequences of up to 8192 rows, 8 key heads x 128, one row each, 128 /
-    // 256 / 512: 190 / 182 / 186 us; 2 prompts of 4096 rows, 8 key heads, eight waves, 128 / 256 / 384 / 512: 194 / 164 / 154
-    // / 155.  fp32 rows take longer: 3 windows of up to 250 rows over 9000, 12 heads x 36, 64 / 80 / 96 / 112 / 160: 98 / 101 /
-    // 103 / 98 / 97; 512 rows over 4096, 32 heads x 128: 325 / 337 / 340 / 339 / 328; 16 sequences of up to 20 rows over 4000, 12 heads x
-    // 36: 64 / 65 / 68 / 69 / 67; 4 of 300 over 2000, 32 heads on 8 x 68: 135 / 129 / 129 / 135 / 140.
+    // What starting an item costs (page ids, queries, first tiles, output), in rows of the cache.  bf16: the prices by which
+    // uneven batches came out lowest: 64 sequences of up to 8192 rows, 8 key heads x 128, one row each, 128 / 256 / 512: 190 / 182
+    // / 186 us; 2 prompts of 4096 rows, 8 key heads, eight waves, 128 / 256 / 384 / 512: 194 / 164 / 154 / 155.  fp32: no price is
+    // ahead of the others by more than where the cuts happen to fall, and 64, the least tried, is taken: 3 windows of up to 250 rows
+    // over 9000, 12 heads x 36, 64 / 80 / 96 / 112 / 160: 98 / 101 / 103 / 98 / 97 us; 512 rows over 4096, 32 heads x 128: 325 / 337
+    // / 340 / 339 / 328; 16 sequences of up to 20 rows over 4000, 12 heads x 36: 64 / 65 / 68 / 69 / 67; 4 of 300 over 2000, 32
+    // heads on 8 x 68: 135 / 129 / 129 / 135 / 140.
     a.start = !bf ? 64 : s.nw == 8 ? 384 : 256;
     a.causal = p->causal != 0;
     a.out_bf16 = p->out_dtype == TLIN_BF16;

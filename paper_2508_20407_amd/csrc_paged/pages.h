@@ -2,8 +2,8 @@
 //
 // A cache's book is small (a table entry a page and sequence, a count a page) and these kernels are bound by the latency of
 // dependent steps, so each does its work in as few launches as its dependences allow: free and fork a workgroup a
-// sequence (counts by integer atomics, whose order changes nothing), reserve one workgroup that scans, compact three
-// launches over the pages (two where there are few).  Copies are bound by HBM.
+// sequence (counts by integer atomics, whose order changes nothing), reserve one workgroup that scans, compact one launch
+// where pages and table entries are few, else two over the pages, beyond 32768 pages three.  Copies are bound by HBM.
 #pragma once
 #include "common.h"
 

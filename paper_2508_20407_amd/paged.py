@@ -285,8 +285,10 @@ def tlin_paged_attn(q, k_pages, v_pages, table, lens, starts, *, max_rows=None, 
                     out=None, return_lse=False, workspace=None):
     """Attention of the new rows q [H,T,D] of every sequence over its rows in the cache: causal, row i of a sequence sees
     the rows up to its own position, else all lens[s] of them.  Query head h reads key head h // (H // HK).  max_rows:
-    most new rows of one sequence, where the program knows it (it picks the kernel's shape, not the result).  Returns O, or
-    (O, lse) with return_lse.  Rows that belong to no sequence are not written."""
+    most new rows of one sequence (it picks the kernel's shape, not the result).  Give it wherever the program knows it: without it
+    all T rows are taken for one sequence's, and a step of many single rows runs in workgroups of up to 256 rows that it leaves
+    almost empty.  Returns O, or (O, lse) with return_lse.  Rows that belong to no sequence are not written.  bf16 caches: weights
+    are rounded to bf16 for the value product, whatever out_dtype is (sums and log-sum-exp are fp32)."""
     dt, index, device = q.dtype, q.get_device(), q.device
     if not (index >= 0 and k_pages.get_device() == v_pages.get_device() == index and k_pages.dtype is dt and v_pages.dtype is dt
             and (out is None or out.get_device() == index)):
