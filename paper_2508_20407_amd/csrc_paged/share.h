@@ -64,7 +64,7 @@ __device__ __forceinline__ ConstPagedArgs *args_again()
 }
 
 // How far a row's logits may exceed its reference point, 8 base-2 units in units of the products.  A number for any scale: an
-// infinite step (scales below 1.7e-38) would leave a reference of -infinity where it is.
+// infinite step (scales below 1.63e-38) would leave a reference of -infinity where it is.
 __device__ __forceinline__ float reference_step(float c) { return fminf(8.0f / c, 3.402823466e38f); }
 
 // Rows that a cut leaves of an item behind it at least.
